@@ -171,6 +171,13 @@ def _marshal(q, k, v, out, lse, stream):
             B, H, N, d), _dtype_code(q), stream
 
 
+def takes_memory(stream: int, device) -> bool:
+    """Whether a call on `stream` may take scratch memory from torch's allocator: it belongs to torch's current stream there and
+    may go back as soon as the kernels are enqueued.  A handle that only the caller knows need not be one queue that outlives its work."""
+    import torch
+    return stream == torch.cuda.current_stream(device).cuda_stream and stream != 2     # 2: hipStreamPerThread, a queue of every thread
+
+
 def attn_fwd(q, k, v, out, lse, causal: bool, scale: float, stream=None) -> None:
     """out, lse <- fused attention forward of device tensors q, k, v ([B,H,N,d]).
     Asynchronous on `stream` (an integer hipStream_t; default: torch's current stream)."""

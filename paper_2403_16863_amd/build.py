@@ -23,7 +23,8 @@ HIPCC_FLAGS = [
 ATTN_PARTS = 9          # parts of the attention variant table (csrc/attn_variants.h)
 
 # (object, source, extra flags)
-UNITS = [("attn_fwd.o", "attn_fwd.hip", []), ("gemm_lrelu.o", "gemm_lrelu.hip", [])] + \
+UNITS = [("attn_fwd.o", "attn_fwd.hip", []), ("gemm_lrelu.o", "gemm_lrelu.hip", []), ("kv4_cache.o", "kv4_cache.hip", []),
+         ("kv4_attn.o", "kv4_attn.hip", []), ("qk_rope.o", "qk_rope.hip", [])] + \
         [(f"attn_kernels_{p}.o", "attn_kernels.hip", [f"-DATTN_PART={p}"]) for p in range(ATTN_PARTS)]
 
 
