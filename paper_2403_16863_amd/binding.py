@@ -122,6 +122,9 @@ def native():
                               "from the repository root") from e
         n.bind(*(ctypes.cast(f, ctypes.c_void_p).value
                  for f in (L.attn_fwd, L.gemm_lrelu_with, L.gemm_lrelu_capturing)))
+        n.bind_cached(*(ctypes.cast(f, ctypes.c_void_p).value
+                        for f in (L.kv4_append, L.kv4_read, L.kv4_attn, L.kv4_attn_workspace, L.qk_norm_rope, L.qk_norm_rope_bwd,
+                                  L.qk_norm_rope_bwd_workspace)))
         _native = n
     return _native
 

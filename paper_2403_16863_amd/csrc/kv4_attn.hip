@@ -409,11 +409,14 @@ __global__ __launch_bounds__(256) void attn_kernel(AttnArgs a) {
     }
 }
 
-// A wave joins the runs of one row (query, head), in their order.
-template <int D, int RB, bool BF>
+// WAVES waves join the runs of one row (query, head): a lane has one run's maximum and sum, then the weighted outputs are added, eight runs'
+// loads at a time (one run after another took 75 us for rows of 128 runs).
+template <int D, int RB, bool BF, int WAVES>
 __global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
-    const int lane = threadIdx.x & 63;
-    const long long vec = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+    constexpr int C = D / 64;
+    __shared__ float part[WAVES > 1 ? 4 : 1][D + 2];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), mine = wave % WAVES;
+    const long long vec = (long long)blockIdx.x * (4 / WAVES) + wave / WAVES;
     if (vec >= (long long)a.T * a.H) return;
     const int t = (int)(vec / a.H), head = (int)(vec % a.H), h = head / a.group;
     int b;
@@ -422,12 +425,11 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
         for (int i = lane; i < a.B; i += 64) upto += a.cu_q[i + 1] <= t;
 #pragma unroll
         for (int d = 32; d; d /= 2) upto += __shfl_xor(upto, d);
-        b = upto;
+        b = __builtin_amdgcn_readfirstlane(upto);
         if (b >= a.B || t < a.cu_q[b]) return;
     } else {
         b = t / a.max_q;
     }
-    b = __builtin_amdgcn_readfirstlane(b);
     const int run = plan<RB>(a);
     const Sequence s = sequence(a, b);
     if (t - s.q0 >= s.nq) return;
@@ -436,22 +438,62 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
     const int runs = runs_of((most + kTile - 1) / kTile, run);
     if (runs == 1) return;
     const int rbs = blocks_of<RB>(a, s);
-    const long long id = first_item<RB>(a, run, b) + (long long)rb * a.heads + h, step = (long long)rbs * a.heads;
+    const long long id = first_item<RB>(a, run, b) + (long long)rb * a.heads + h, step = (long long)rbs * a.heads * RB * (D + 2);
     const float* from = a.ws + (id * RB + row % RB) * (D + 2);
-    float top = -INFINITY, sum = 0, o[D / 64] = {};
-    for (int r = 0; r < runs; ++r) top = fmaxf(top, from[r * step * RB * (D + 2) + D]);
-    const float ref = top == -INFINITY ? 0.f : top;
-    for (int r = 0; r < runs; ++r) {
-        const float* p = from + r * step * RB * (D + 2);
-        const float by = __builtin_amdgcn_exp2f(p[D] - ref);
-        sum += p[D + 1] * by;
+    // Lane l has run r0 + WAVES l: its reference is raised for 64 runs at a time.
+    float top = -INFINITY, sum = 0, o[C] = {};
+    for (int r0 = mine; r0 < runs; r0 += 64 * WAVES) {
+        const int r = r0 + WAVES * lane;
+        float m = -INFINITY, l = 0;
+        if (r < runs) m = from[r * step + D], l = from[r * step + D + 1];
+        float to = m;
 #pragma unroll
-        for (int i = 0; i < D / 64; ++i) o[i] += p[lane * (D / 64) + i] * by;
+        for (int d = 32; d; d /= 2) to = fmaxf(to, __shfl_xor(to, d));
+        to = fmaxf(to, top);
+        const float ref = to == -INFINITY ? 0.f : to, by = __builtin_amdgcn_exp2f(top - ref);
+        const float weight = __builtin_amdgcn_exp2f(m - ref);
+        top = to;
+        sum = sum * by + weight * l;  // each lane's own runs
+        for (int i = 0; i < C; ++i) o[i] *= by;
+        const int n = min(64, (runs - r0 + WAVES - 1) / WAVES);
+        for (int k = 0; k < n; k += 8) {
+            float x[8][C];
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+#pragma unroll
+                for (int i = 0; i < C; ++i) x[u][i] = from[(r0 + WAVES * min(k + u, n - 1)) * step + lane * C + i];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const float w = __shfl(weight, min(k + u, n - 1));
+#pragma unroll
+                for (int i = 0; i < C; ++i)
+                    if (k + u < n) o[i] += x[u][i] * w;
+            }
+        }
+    }
+#pragma unroll
+    for (int d = 32; d; d /= 2) sum += __shfl_xor(sum, d);
+    if constexpr (WAVES > 1) {
+#pragma unroll
+        for (int i = 0; i < C; ++i) part[wave][lane * C + i] = o[i];
+        if (lane == 0) part[wave][D] = top, part[wave][D + 1] = sum;
+        __syncthreads();
+        if (wave) return;
+        top = -INFINITY;
+        for (int w = 0; w < WAVES; ++w) top = fmaxf(top, part[w][D]);
+        const float ref = top == -INFINITY ? 0.f : top;
+        sum = 0;
+        for (int i = 0; i < C; ++i) o[i] = 0;
+        for (int w = 0; w < WAVES; ++w) {
+            const float by = __builtin_amdgcn_exp2f(part[w][D] - ref);
+            sum += part[w][D + 1] * by;
+            for (int i = 0; i < C; ++i) o[i] += part[w][lane * C + i] * by;
+        }
     }
     const float by = sum == 0.f ? 0.f : 1.f / sum;
     if (lane == 0) a.lse[vec] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
     if (D == 128) {
-        *(unsigned*)(a.out + vec * D + 2 * lane) = pack2<BF>(o[0] * by, o[D / 64 - 1] * by);
+        *(unsigned*)(a.out + vec * D + 2 * lane) = pack2<BF>(o[0] * by, o[C - 1] * by);
     } else {
         a.out[vec * D + lane] = (uint16_t)pack2<BF>(o[0] * by, 0.f);
     }
@@ -489,12 +531,15 @@ int launch_attn(const Choice& c, AttnArgs& a, void* stream) {
     const void* fn = c.nt == 1   ? (const void*)attn_kernel<D, 1, BF>
                      : c.nt == 2 ? (const void*)attn_kernel<D, 2, BF>
                                  : (const void*)attn_kernel<D, 4, BF>;
-    const void* join = c.nt == 1   ? (const void*)join_kernel<D, 16, BF>
-                       : c.nt == 2 ? (const void*)join_kernel<D, 32, BF>
-                                   : (const void*)join_kernel<D, 64, BF>;
+    // Rows enough to fill the units get a wave each, fewer ones a workgroup: those are the rows with many runs.
+    const long long rows = (long long)a.T * a.H;
+    const bool many = rows >= 4096;
+    const void* join = c.nt == 1   ? (many ? (const void*)join_kernel<D, 16, BF, 1> : (const void*)join_kernel<D, 16, BF, 4>)
+                       : c.nt == 2 ? (many ? (const void*)join_kernel<D, 32, BF, 1> : (const void*)join_kernel<D, 32, BF, 4>)
+                                   : (many ? (const void*)join_kernel<D, 64, BF, 1> : (const void*)join_kernel<D, 64, BF, 4>);
     void* list[] = {&a};
     if (hipLaunchKernel(fn, dim3((unsigned)c.blocks), dim3(256), list, 0, (hipStream_t)stream) != hipSuccess ||
-        (a.ws && hipLaunchKernel(join, dim3((unsigned)(((long long)a.T * a.H + 3) / 4)), dim3(256), list, 0, (hipStream_t)stream) != hipSuccess)) {
+        (a.ws && hipLaunchKernel(join, dim3((unsigned)(many ? (rows + 3) / 4 : rows)), dim3(256), list, 0, (hipStream_t)stream) != hipSuccess)) {
         (void)hipGetLastError();
         return KV4_ELAUNCH;
     }

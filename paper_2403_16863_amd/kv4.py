@@ -99,11 +99,29 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+def _first(name):
+    """The native module's function of that name, from the first call on (one lookup a call)."""
+    def first(*args):
+        lib()
+        globals()["_plain_" + name] = call = getattr(binding.native(), "kv4_" + name)
+        return call(*args)
+    return first
+
+
+_plain_append, _plain_read, _plain_attn = _first("append"), _first("read"), _first("attn")
+
+
 def kv4_append(k, v, cache, slots, cos=None, sin=None, positions=None, interleaved: bool = False, stream=None) -> None:
     """Slot slots[t] of the cache <- k[t], rotated by positions[t], and v[t], for k and v [T,heads,d] (any strides that divide by
     8, channels contiguous).  Tokens whose slot lies outside the cache (-1: padding) are left out; the others' slots must
     differ.  cos, sin: float32 [rows,d/2], or None for keys that need no rotation (any more).  Asynchronous on `stream` (an
     integer hipStream_t; default: torch's current stream)."""
+    rc = _plain_append(k, v, cache, slots, cos, sin, positions, interleaved, stream)
+    if not rc:
+        return
+    if rc < 0:
+        raise Kv4Error(rc, "kv4_append")
+    # not a plain call: the steps one by one, each of which says what it refuses
     import torch
     _devices(cache, (("cache", cache), ("k", k), ("v", v), ("slots", slots), ("cos", cos), ("sin", sin), ("positions", positions)))
     pages, heads, page_size, d = _cache(cache)
@@ -135,6 +153,12 @@ def kv4_append(k, v, cache, slots, cos=None, sin=None, positions=None, interleav
 
 def kv4_read(cache, slots, k=None, v=None, stream=None) -> None:
     """k, v [T,heads,d] (contiguous; either may be None) <- what slot slots[t] of the cache holds, zeros for a slot outside it."""
+    rc = _plain_read(cache, slots, k, v, stream)
+    if not rc:
+        return
+    if rc < 0:
+        raise Kv4Error(rc, "kv4_read")
+    # not a plain call: the steps one by one, each of which says what it refuses
     import torch
     like = k if k is not None else v
     if like is None:
@@ -172,7 +196,14 @@ def kv4_attn(q, cache, tables, lens, out, lse, causal: bool, scale: float, cu_q=
 
     Few long sequences are cut into runs of keys for which the call needs scratch memory: `workspace` (uint8,
     kv4_attn_workspace bytes), or, on torch's current stream, memory that it takes from torch's allocator itself (the graph's own
-    pool while torch records one).  On another stream without a workspace the keys are not cut, which is slower."""
+    pool while torch records one; recordings begun elsewhere need the argument).  On another stream without a workspace the keys are
+    not cut, which is slower."""
+    rc = _plain_attn(q, cache, tables, lens, out, lse, causal, scale, cu_q, max_q, workspace, stream)
+    if not rc:
+        return
+    if rc < 0:
+        raise Kv4Error(rc, "kv4_attn")
+    # not a plain call: the steps one by one, each of which says what it refuses
     import torch
     _devices(cache, (("cache", cache), ("q", q), ("tables", tables), ("lens", lens), ("out", out), ("lse", lse), ("cu_q", cu_q),
                      ("workspace", workspace)))

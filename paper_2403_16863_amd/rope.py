@@ -102,12 +102,30 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+def _first(name):
+    """The native module's function of that name, from the first call on (one lookup a call)."""
+    def first(*args):
+        lib()
+        globals()["_plain_" + name] = call = getattr(binding.native(), "qk_" + name)
+        return call(*args)
+    return first
+
+
+_plain_norm_rope, _plain_norm_rope_bwd = _first("norm_rope"), _first("norm_rope_bwd")
+
+
 def qk_norm_rope(q, k, q_out, k_out, cos, sin, positions, q_weight=None, k_weight=None, eps: float = 1e-6, interleaved: bool = False,
                  stream=None) -> None:
     """q_out, k_out <- norm (where there is a weight) and rotation of q [B,N,H,d] and k [B,N,Hkv,d].  All four may have any
     strides that divide by 8 with contiguous channels: slices of a joint projection, or the transposed view of attn_fwd's [B,H,N,d];
     q or k may be None with its output.  cos, sin: float32 [rows,d/2]; positions: int32 [B,N].  Asynchronous on `stream` (an
     integer hipStream_t; default: torch's current stream)."""
+    rc = _plain_norm_rope(q, k, q_out, k_out, cos, sin, positions, q_weight, k_weight, eps, interleaved, stream)
+    if not rc:
+        return
+    if rc < 0:
+        raise RopeError(rc, "qk_norm_rope")
+    # not a plain call: the steps one by one, each of which says what it refuses
     import torch
     like = q if q is not None else k
     if like is None or (q is None) != (q_out is None) or (k is None) != (k_out is None):
@@ -140,7 +158,15 @@ def qk_norm_rope_bwd(dq_out, dk_out, q, k, dq, dk, cos, sin, positions, q_weight
     """dq, dk, dq_weight, dk_weight <- gradients of qk_norm_rope, from those of its outputs and its inputs q, k (not needed, and
     None will do, for a tensor without a weight).  dq_weight, dk_weight: float32 [d], written.  With a weight
     the call needs scratch memory: `workspace` (uint8, qk_norm_rope_bwd_workspace bytes), or, on torch's current stream,
-    memory that it takes from torch's allocator itself (the graph's own pool while torch records one)."""
+    memory that it takes from torch's allocator itself (the graph's own pool while torch records one; recordings begun
+    elsewhere need the argument)."""
+    rc = _plain_norm_rope_bwd(dq_out, dk_out, q, k, dq, dk, cos, sin, positions, q_weight, k_weight, dq_weight, dk_weight, eps, interleaved,
+                              workspace, stream)
+    if not rc:
+        return
+    if rc < 0:
+        raise RopeError(rc, "qk_norm_rope_bwd")
+    # not a plain call: the steps one by one, each of which says what it refuses
     import torch
     like = dq_out if dq_out is not None else dk_out
     if like is None or (dq_out is None) != (dq is None) or (dk_out is None) != (dk is None):
