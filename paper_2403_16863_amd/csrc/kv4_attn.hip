@@ -60,6 +60,13 @@ __device__ __forceinline__ Sequence sequence(const AttnArgs& a, int b) {
     return s;
 }
 
+// The same for a sequence that all lanes share: what follows from it stays in scalar registers.
+__device__ __forceinline__ Sequence shared_sequence(const AttnArgs& a, int b) {
+    Sequence s = sequence(a, b);
+    s.len = __builtin_amdgcn_readfirstlane(s.len), s.q0 = __builtin_amdgcn_readfirstlane(s.q0), s.nq = __builtin_amdgcn_readfirstlane(s.nq);
+    return s;
+}
+
 __device__ __forceinline__ int wave_sum_scan(int x) {  // inclusive prefix sum over the 64 lanes
     const int lane = threadIdx.x & 63;
 #pragma unroll
@@ -80,7 +87,7 @@ __device__ __forceinline__ int runs_of(int tiles, int run) { return max(1, (tile
 // Tiles of a run: all (sequence, row block, head) together make about `target` runs, none shorter than kMinTiles.
 template <int RB>
 __device__ __forceinline__ int plan(const AttnArgs& a) {
-    if (!a.ws) return INT_MAX / 2;
+    if (!a.ws) return INT_MAX / 2;  // no runs
     const int lane = threadIdx.x & 63;
     long long all = 0;
     for (int b = lane; b < a.B; b += 64) {
@@ -135,27 +142,30 @@ __device__ __forceinline__ int keys_of(const AttnArgs& a, const Sequence& s, int
     return a.causal ? max(0, s.len - s.nq + row / a.group + 1) : s.len;
 }
 
-// One tile's bytes of one lane.
+// One tile's bytes of one lane: [group of 16 tokens][words].
 template <int D>
 struct Raw {
-    unsigned k[2][D / 32], v[2][D / 32];  // [group of 16 tokens][words]
+    unsigned k[2][D / 32], v[2][D / 32];
     unsigned ks[2], vs[2];
 };
 
-template <int D, int NT, bool BF>
-__global__ __launch_bounds__(256) void attn_kernel(AttnArgs a) {
+// Indices that the launch only reads, through the scalar cache.
+typedef const int __attribute__((address_space(4))) * const_ints;
+
+template <int D, int NT, int NW, bool BF>
+__global__ __launch_bounds__(64 * NW, NW / 4 * (NT == 1 ? 4 : NT == 2 ? 2 : 1)) void attn_kernel(AttnArgs a) {
     constexpr int RB = 16 * NT, KS = D / 32, CT = D / 16, W = D / 32;
-    __shared__ float joined[2][CT * NT][64 * 4];
-    __shared__ float stats[4][RB][2];
+    __shared__ float joined[NW / 2][CT * NT][64 * 4];
+    __shared__ float stats[NW][RB][2];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quad = lane >> 4;
 
-    const int run = plan<RB>(a);
+    const int run = __builtin_amdgcn_readfirstlane(plan<RB>(a));
     int b = 0;
     long long first = 0;
     const long long id = blockIdx.x;
     if (!find_item<RB>(a, run, id, b, first)) return;
     b = __builtin_amdgcn_readfirstlane(b);
-    const Sequence s = sequence(a, b);
+    const Sequence s = shared_sequence(a, b);
     const int rbs = blocks_of<RB>(a, s);
     int rest = __builtin_amdgcn_readfirstlane((int)(id - first));
     const int h = rest % a.heads;
@@ -166,6 +176,36 @@ __global__ __launch_bounds__(256) void attn_kernel(AttnArgs a) {
     const int tiles = (most + kTile - 1) / kTile, runs = runs_of(tiles, run);
     if (r >= runs) return;  // these rows see fewer keys than the sequence has
     const int t0 = r * run, t1 = min(tiles, t0 + run);
+
+    const const_ints table = (const_ints)(uintptr_t)(a.tables + (long long)b * a.width);
+    const int groups_page = 1 << (a.page_shift - 4);
+    // Group g's (16 tokens') page; groups behind the last one stand for that one (their keys are masked).
+    const int last_group = max(0, (most + 15) / 16 - 1);
+    auto page_of = [&](int g) { return table[min(g, last_group) >> (a.page_shift - 4)]; };
+    auto group_at = [&](int g, int page) {
+        const int p = (unsigned)page < (unsigned)a.pages ? page : 0;
+        return a.cache + (((long long)p * a.heads + h) * groups_page + (min(g, last_group) & (groups_page - 1))) * Group<D>::bytes;
+    };
+    Raw<D> raw;
+    auto fetch_k = [&](const uint8_t* at, int i) {
+        const unsigned* k = (const unsigned*)(at + col * (D / 2) + quad * (D / 8));
+#pragma unroll
+        for (int w = 0; w < W; ++w) raw.k[i][w] = k[w];
+        raw.ks[i] = at[Group<D>::k_scales + col * (D / 32) + quad * (D / 4) / 32];
+    };
+    auto fetch_v = [&](const uint8_t* at, int i) {
+        const unsigned* v = (const unsigned*)(at + Group<D>::v_codes + quad * (2 * D) + col * (D / 8));
+#pragma unroll
+        for (int w = 0; w < W; ++w) raw.v[i][w] = v[w];
+        raw.vs[i] = *(const unsigned*)(at + Group<D>::v_scales + quad * (D / 8) + col * (D / 16) / 32 * 4);
+    };
+    // The first tile's bytes, and the pages of the second, are under way before the queries are asked for.
+    int t = t0 + wave, pages[2] = {-1, -1}, ahead[2] = {-1, -1};
+    if (t < t1) {
+        for (int i = 0; i < 2; ++i) pages[i] = page_of(2 * t + i), ahead[i] = page_of(2 * (t + NW) + i);
+        for (int i = 0; i < 2; ++i) fetch_k(group_at(2 * t + i, pages[i]), i);
+        for (int i = 0; i < 2; ++i) fetch_v(group_at(2 * t + i, pages[i]), i);
+    }
 
     // Queries: row col of tile n, channels quad * D/4 + 8 ks .. + 7.
     f16x8 q[NT][KS];
@@ -199,22 +239,6 @@ __global__ __launch_bounds__(256) void attn_kernel(AttnArgs a) {
             for (int i = 0; i < 8; ++i) q[n][k][i] = (_Float16)(BF ? ldexpf(x[k][i], -e) : x[k][i]);
     }
 
-    const int* table = a.tables + (long long)b * a.width;
-    const int groups_page = 1 << (a.page_shift - 4);
-    // Group g's (16 tokens') page, or -1; groups behind the last one stand for that one (their keys are masked).
-    const int last_group = max(0, (most + 15) / 16 - 1);
-    auto page_of = [&](int g) { return most > 0 ? table[min(g, last_group) >> (a.page_shift - 4)] : -1; };
-    auto fetch = [&](int g, int page, int i, Raw<D>& raw) {
-        const int p = (unsigned)page < (unsigned)a.pages ? page : 0;
-        const uint8_t* at = a.cache + (((long long)p * a.heads + h) * groups_page + (min(g, last_group) & (groups_page - 1))) * Group<D>::bytes;
-        const unsigned* k = (const unsigned*)(at + col * (D / 2) + quad * (D / 8));
-        const unsigned* v = (const unsigned*)(at + Group<D>::v_codes + quad * (2 * D) + col * (D / 8));
-#pragma unroll
-        for (int w = 0; w < W; ++w) raw.k[i][w] = k[w], raw.v[i][w] = v[w];
-        raw.ks[i] = at[Group<D>::k_scales + col * (D / 32) + quad * (D / 4) / 32];
-        raw.vs[i] = *(const unsigned*)(at + Group<D>::v_scales + quad * (D / 8) + col * (D / 16) / 32 * 4);
-    };
-
     f32x4 o[NT][CT];
     float m[NT], l[NT];
 #pragma unroll
@@ -224,20 +248,8 @@ __global__ __launch_bounds__(256) void attn_kernel(AttnArgs a) {
         for (int c = 0; c < CT; ++c) o[n][c] = {0, 0, 0, 0};
     }
 
-    Raw<D> next;
-    int pages[2] = {-1, -1};
-    int t = t0 + wave;
-    if (t < t1) {
-        for (int i = 0; i < 2; ++i) pages[i] = page_of(2 * t + i);
-        for (int i = 0; i < 2; ++i) fetch(2 * t + i, pages[i], i, next);
-    }
-    for (; t < t1; t += 4) {
-        Raw<D> now = next;
+    for (; t < t1; t += NW) {
         const bool there[2] = {(unsigned)pages[0] < (unsigned)a.pages, (unsigned)pages[1] < (unsigned)a.pages};
-        if (t + 4 < t1) {
-            for (int i = 0; i < 2; ++i) pages[i] = page_of(2 * (t + 4) + i);
-            for (int i = 0; i < 2; ++i) fetch(2 * (t + 4) + i, pages[i], i, next);
-        }
         const bool masked = (t + 1) * kTile > least || !there[0] || !there[1];
 
         float x[NT][8];
@@ -248,7 +260,7 @@ __global__ __launch_bounds__(256) void attn_kernel(AttnArgs a) {
             for (int n = 0; n < NT; ++n) acc[n] = {0, 0, 0, 0};
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
-                const uint4 w = values8<false>(now.k[i][k], now.ks[i] << 23);
+                const uint4 w = values8<false>(raw.k[i][k], raw.ks[i] << 23);
                 const f16x8 f = __builtin_bit_cast(f16x8, w);
 #pragma unroll
                 for (int n = 0; n < NT; ++n) acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, q[n][k], acc[n], 0, 0, 0);
@@ -258,6 +270,14 @@ __global__ __launch_bounds__(256) void attn_kernel(AttnArgs a) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) x[n][4 * i + j] = acc[n][j] * factor[n];
         }
+        // The next tile's keys take the registers of this one's (behind the run's end: the last group's once more).
+        const uint8_t* next[2];
+        for (int i = 0; i < 2; ++i) {
+            pages[i] = ahead[i];
+            next[i] = group_at(2 * (t + NW) + i, pages[i]);
+            fetch_k(next[i], i);
+            ahead[i] = page_of(2 * (t + 2 * NW) + i);
+        }
         if (masked) {
 #pragma unroll
             for (int i = 0; i < 2; ++i)
@@ -266,14 +286,14 @@ __global__ __launch_bounds__(256) void attn_kernel(AttnArgs a) {
                     const int key = t * kTile + 16 * i + 4 * quad + j;
                     // Values that some row of the block does not see must not reach it as 0 * NaN: a NaN among them goes into the
                     // scores of the rows that do see it, and the codes that nobody sees are cleared with it.
-                    const unsigned byte = now.vs[i] << (24 - 8 * j) >> 24;
+                    const unsigned byte = raw.vs[i] << (24 - 8 * j) >> 24;
                     const unsigned long long bad = __ballot(byte == 255u);
                     const bool nan = (bad >> (16 * quad) & 0xffffu) != 0;
                     const bool dead = nan || key >= most || !there[i];
                     if (dead) {
-                        if (D == 128) now.v[i][j % W] = 0;
-                        else now.v[i][j / 2] &= j % 2 ? 0xffffu : 0xffff0000u;
-                        now.vs[i] = (now.vs[i] & ~(0xffu << (8 * j))) | 127u << (8 * j);
+                        if (D == 128) raw.v[i][j % W] = 0;
+                        else raw.v[i][j / 2] &= j % 2 ? 0xffffu : 0xffff0000u;
+                        raw.vs[i] = (raw.vs[i] & ~(0xffu << (8 * j))) | 127u << (8 * j);
                     }
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
@@ -310,7 +330,7 @@ __global__ __launch_bounds__(256) void attn_kernel(AttnArgs a) {
         unsigned sc[2][4];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            sc[i][0] = now.vs[i] << 23, sc[i][1] = now.vs[i] << 15, sc[i][2] = now.vs[i] << 7, sc[i][3] = now.vs[i] >> 1;
+            sc[i][0] = raw.vs[i] << 23, sc[i][1] = raw.vs[i] << 15, sc[i][2] = raw.vs[i] << 7, sc[i][3] = raw.vs[i] >> 1;
         }
         auto channels = [&](auto SEL) {
             constexpr int c = decltype(SEL)::value;  // channels 2c and 2c + 1 of the lane's run
@@ -319,12 +339,12 @@ __global__ __launch_bounds__(256) void attn_kernel(AttnArgs a) {
             for (int i = 0; i < 2; ++i) {
                 if constexpr (D == 128) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) two[i][j] = values2<false, c>(now.v[i][j % W], sc[i][j]);
+                    for (int j = 0; j < 4; ++j) two[i][j] = values2<false, c>(raw.v[i][j % W], sc[i][j]);
                 } else {
-                    two[i][0] = values2<false, c>(now.v[i][0], sc[i][0]);
-                    two[i][1] = values2<false, 2 + c>(now.v[i][0], sc[i][1]);
-                    two[i][2] = values2<false, c>(now.v[i][1], sc[i][2]);
-                    two[i][3] = values2<false, 2 + c>(now.v[i][1], sc[i][3]);
+                    two[i][0] = values2<false, c>(raw.v[i][0], sc[i][0]);
+                    two[i][1] = values2<false, 2 + c>(raw.v[i][0], sc[i][1]);
+                    two[i][2] = values2<false, c>(raw.v[i][1], sc[i][2]);
+                    two[i][3] = values2<false, 2 + c>(raw.v[i][1], sc[i][3]);
                 }
             }
             uint4 even, odd;
@@ -337,6 +357,7 @@ __global__ __launch_bounds__(256) void attn_kernel(AttnArgs a) {
                 o[n][2 * c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, even), p[n], o[n][2 * c], 0, 0, 0);
                 o[n][2 * c + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, odd), p[n], o[n][2 * c + 1], 0, 0, 0);
             }
+            if (NT == 1) __builtin_amdgcn_sched_barrier(0);  // a few channels at a time: all of them at once would not fit 128 registers
         };
         channels(std::integral_constant<int, 0>());
         channels(std::integral_constant<int, 1>());
@@ -344,9 +365,10 @@ __global__ __launch_bounds__(256) void attn_kernel(AttnArgs a) {
             channels(std::integral_constant<int, 2>());
             channels(std::integral_constant<int, 3>());
         }
+        for (int i = 0; i < 2; ++i) fetch_v(next[i], i);
     }
 
-    // The waves meet: a common reference for each row, then 3 -> 1 and 2 -> 0, then 1 -> 0.
+    // The waves meet: a common reference for each row, then the upper half's outputs go to the lower half, until one is left.
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         l[n] += __shfl_xor(l[n], 16);
@@ -357,16 +379,18 @@ __global__ __launch_bounds__(256) void attn_kernel(AttnArgs a) {
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         float top = -INFINITY, sum = 0;
-        for (int w = 0; w < 4; ++w) top = fmaxf(top, stats[w][16 * n + col][0]);
+#pragma unroll
+        for (int w = 0; w < NW; ++w) top = fmaxf(top, stats[w][16 * n + col][0]);
         const float ref = top == -INFINITY ? 0.f : top;
-        for (int w = 0; w < 4; ++w) sum += stats[w][16 * n + col][1] * __builtin_amdgcn_exp2f(stats[w][16 * n + col][0] - ref);
+#pragma unroll
+        for (int w = 0; w < NW; ++w) sum += stats[w][16 * n + col][1] * __builtin_amdgcn_exp2f(stats[w][16 * n + col][0] - ref);
         const float by = __builtin_amdgcn_exp2f(m[n] - ref);
         m[n] = top, l[n] = sum;
 #pragma unroll
         for (int c = 0; c < CT; ++c) o[n][c] *= by;
     }
 #pragma unroll
-    for (int half = 2; half; half /= 2) {
+    for (int half = NW / 2; half; half /= 2) {
         if (wave >= half && wave < 2 * half)
 #pragma unroll
             for (int n = 0; n < NT; ++n)
@@ -378,7 +402,7 @@ __global__ __launch_bounds__(256) void attn_kernel(AttnArgs a) {
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int c = 0; c < CT; ++c) o[n][c] += *(const f32x4*)&joined[wave][n * CT + c][4 * lane];
-        __syncthreads();
+        if (half > 1) __syncthreads();
     }
     if (wave) return;
 #pragma unroll
@@ -430,8 +454,8 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
     } else {
         b = t / a.max_q;
     }
-    const int run = plan<RB>(a);
-    const Sequence s = sequence(a, b);
+    const int run = __builtin_amdgcn_readfirstlane(plan<RB>(a));
+    const Sequence s = shared_sequence(a, b);
     if (t - s.q0 >= s.nq) return;
     const int row = (t - s.q0) * a.group + head % a.group, rb = row / RB, rows = s.nq * a.group;
     const int most = keys_of(a, s, min((rb + 1) * RB, rows) - 1);
@@ -500,10 +524,11 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
 }
 
 struct Choice {
-    int nt, target;
+    int nt, nw, target;
     long long blocks, bytes;
 };
 
+constexpr int kShort = 2048;   // keys
 constexpr int kTarget = 1024;  // runs of a launch: four workgroups on each of 256 units
 
 Choice choose(int B, int heads, int group, int d, long long cap, int max_q) {
@@ -512,7 +537,9 @@ Choice choose(int B, int heads, int group, int d, long long cap, int max_q) {
     c.nt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
     c.target = kTarget;
     const long long rbs = (rows + 16 * c.nt - 1) / (16 * c.nt), alone = B * rbs * heads;
-    const bool one = cap <= (long long)kTile * kMinTiles;  // no sequence has more than one run
+    // Sequences that cannot be long are not cut: 16 waves go over up to four tiles each, and there is nothing to join.
+    const bool one = cap <= kShort;
+    c.nw = one && c.nt == 1 ? 16 : 4;
     c.blocks = one ? alone : alone + c.target;
     c.bytes = one ? 0 : c.blocks * 16 * c.nt * (d + 2) * 4;
     return c;
@@ -528,9 +555,10 @@ int check_sizes(int B, int H, int heads, int d, int page_size, int width, int ma
 
 template <int D, bool BF>
 int launch_attn(const Choice& c, AttnArgs& a, void* stream) {
-    const void* fn = c.nt == 1   ? (const void*)attn_kernel<D, 1, BF>
-                     : c.nt == 2 ? (const void*)attn_kernel<D, 2, BF>
-                                 : (const void*)attn_kernel<D, 4, BF>;
+    const void* fn = c.nw == 16  ? (const void*)attn_kernel<D, 1, 16, BF>
+                     : c.nt == 1 ? (const void*)attn_kernel<D, 1, 4, BF>
+                     : c.nt == 2 ? (const void*)attn_kernel<D, 2, 4, BF>
+                                 : (const void*)attn_kernel<D, 4, 4, BF>;
     // Rows enough to fill the units get a wave each, fewer ones a workgroup: those are the rows with many runs.
     const long long rows = (long long)a.T * a.H;
     const bool many = rows >= 4096;
@@ -538,7 +566,7 @@ int launch_attn(const Choice& c, AttnArgs& a, void* stream) {
                        : c.nt == 2 ? (many ? (const void*)join_kernel<D, 32, BF, 1> : (const void*)join_kernel<D, 32, BF, 4>)
                                    : (many ? (const void*)join_kernel<D, 64, BF, 1> : (const void*)join_kernel<D, 64, BF, 4>);
     void* list[] = {&a};
-    if (hipLaunchKernel(fn, dim3((unsigned)c.blocks), dim3(256), list, 0, (hipStream_t)stream) != hipSuccess ||
+    if (hipLaunchKernel(fn, dim3((unsigned)c.blocks), dim3(64 * c.nw), list, 0, (hipStream_t)stream) != hipSuccess ||
         (a.ws && hipLaunchKernel(join, dim3((unsigned)(many ? (rows + 3) / 4 : rows)), dim3(256), list, 0, (hipStream_t)stream) != hipSuccess)) {
         (void)hipGetLastError();
         return KV4_ELAUNCH;
