@@ -74,9 +74,10 @@ int kv4_read(const void* cache, const int* slots, void* k, void* v, int T, int h
  *  max_q  : the largest number of queries of a sequence (cu_q null: T / B); an upper bound will do, but costs workgroups.
  *  workspace : device, 16-byte aligned, kv4_attn_workspace bytes, any contents, not used by anybody else until the call's
  *           kernels have run; null or fewer bytes: each workgroup goes over all keys of its rows, which is slower for few
- *           long sequences.
+ *           long sequences or unequal ones.
  *  Limits (KV4_EUNSUPPORTED): pages * page_size and width * page_size <= 2^31 - 1, T * H <= 2^31 - 1, H / heads * max_q <= 2^30,
- *           B <= 65535, fewer than 2^23 workgroups.
+ *           B <= 65535, fewer than 2^23 workgroups (16 to 64 rows of a sequence and head each), and these times width * page_size / 32 below 2^31 where
+ *           there is a use for a workspace.
  *
  * Accuracy: products of 16-bit values (bfloat16 queries become binary16 relative to the row's largest) and of the cache's values in fp32, the probabilities
  * are rounded to binary16 before the second product, and out once at the end.  |out - exact| <= u |out| + 2^-11 sum_j p_j |v_j| + small
@@ -89,7 +90,7 @@ int kv4_attn(const void* q, const void* cache, const int* tables, const int* len
              void* workspace, long long workspace_bytes, void* stream);
 
 /* The bytes of scratch memory that kv4_attn has a use for (0: none); negative: the error that the call would give. */
-long long kv4_attn_workspace(int B, int H, int heads, int d, int page_size, int width, int max_q);
+long long kv4_attn_workspace(int T, int B, int H, int heads, int d, int page_size, int width, int max_q);
 
 const char* kv4_strerror(int code);
 

@@ -13,7 +13,9 @@
 // the power of two of their row's largest element.
 //
 // The keys of all sequences are dealt on the device, from the lengths that the launch finds in memory (a captured launch meets new ones
-// at every replay): `plan` picks the tiles of a run so that all runs together are about `target`, and a second kernel joins the runs of a row.
+// at every replay).  A segment is a sequence, a block of rows and a head; all segments' tiles on end are cut into ranges of one length, one for
+// each workgroup, wherever that falls, so that workgroups end together however unequal the sequences are; a second
+// kernel joins the pieces of a row.  Where no sequence is long, workgroups take whole segments instead.
 #include <hip/hip_runtime.h>
 #include <limits.h>
 #include <math.h>
@@ -26,6 +28,7 @@ namespace kv4 {
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 struct AttnArgs {
     const uint16_t* q;
@@ -33,15 +36,18 @@ struct AttnArgs {
     const int *tables, *lens, *cu_q;
     uint16_t* out;
     float* lse;
-    float* ws;  // partial outputs, then maxima and sums; null: no runs, each workgroup takes all keys
+    int2* heads_ws;  // of each row: its first piece's row in ws, its pieces; null: no scratch memory, whole segments only
+    float* ws;       // pieces' rows: output, maximum, sum
     int T, B, H, heads, group, pages, page_shift, width, max_q, causal;
     float scale_l2;  // scale * log2(e)
-    int target;      // runs that the launch is to be cut into
+    int target;      // ranges that a launch is cut into at most
 };
 
-constexpr int kTile = 32;     // keys of a step of one wave
-constexpr int kMinTiles = 4;  // a run's tiles at least: one for each wave
-constexpr float kRaise = 8;   // scores (in powers of two) by which a row may pass its reference before that is raised: P < 2^8 in binary16
+constexpr int kTile = 32;      // keys of a step of one wave
+constexpr int kMinRange = 16;  // tiles of a range at least: four for each wave
+constexpr int kBegin = 8;      // what it costs a workgroup to begin and end a segment, in tiles (about 5 us)
+constexpr int kWhole = 48;         // tiles up to which a segment is left whole if no other is longer
+constexpr float kRaise = 8;    // scores (in powers of two) by which a row may pass its reference before that is raised: P < 2^8 in binary16
 
 struct Sequence {
     int len, q0, nq;
@@ -67,13 +73,14 @@ __device__ __forceinline__ Sequence shared_sequence(const AttnArgs& a, int b) {
     return s;
 }
 
-__device__ __forceinline__ int wave_sum_scan(int x) {  // inclusive prefix sum over the 64 lanes
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const int y = __shfl_up(x, d);
-        if (lane >= d) x += y;
-    }
+// Inclusive prefix sum over the 64 lanes, in the rows of 16 first.
+__device__ __forceinline__ int prefix_sum(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // row_shr 1, 2, 4, 8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast 15, 31
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
     return x;
 }
 
@@ -81,60 +88,67 @@ template <int RB>
 __device__ __forceinline__ int blocks_of(const AttnArgs& a, const Sequence& s) {
     return (s.nq * a.group + RB - 1) / RB;
 }
-__device__ __forceinline__ int tiles_of(const Sequence& s) { return (s.len + kTile - 1) / kTile; }
-__device__ __forceinline__ int runs_of(int tiles, int run) { return max(1, (tiles + run - 1) / run); }
+// Positions of a segment: kBegin and then its tiles; one without keys has its rows to write and counts as one tile.
+template <class F>
+__device__ __forceinline__ int positions_of(const Sequence& s) { return kBegin + max(1, (s.len + F::tile - 1) / F::tile); }
 
-// Tiles of a run: all (sequence, row block, head) together make about `target` runs, none shorter than kMinTiles.
-template <int RB>
-__device__ __forceinline__ int plan(const AttnArgs& a) {
-    if (!a.ws) return INT_MAX / 2;  // no runs
-    const int lane = threadIdx.x & 63;
-    long long all = 0;
-    for (int b = lane; b < a.B; b += 64) {
-        const Sequence s = sequence(a, b);
-        all += (long long)tiles_of(s) * blocks_of<RB>(a, s);
-    }
-#pragma unroll
-    for (int d = 32; d; d /= 2) all += __shfl_xor(all, d);
-    return (int)max((long long)kMinTiles, (all * a.heads + a.target - 1) / a.target);
-}
+// Where a workgroup begins.
+struct Start {
+    int range;   // tiles of a range; 0: whole segments
+    int b;       // the sequence
+    int first;   // position of its first segment
+    int before;  // segments of the sequences before it
+    int total;   // positions of all
+    Sequence s;
+};
 
-// The sequence that item `id` of the launch belongs to, and the id of that sequence's first item; false: there is no such item.
-template <int RB>
-__device__ __forceinline__ bool find_item(const AttnArgs& a, int run, long long id, int& b, long long& first) {
+template <class F>
+__device__ __forceinline__ bool start_of(const AttnArgs& a, int id, Start& at) {
     const int lane = threadIdx.x & 63;
-    long long before = 0;
+    int all = 0, longest = 0, segments = 0, tiles = 0;
+    Sequence s = {};
     for (int b0 = 0; b0 < a.B; b0 += 64) {
-        int n = 0;
+        segments = tiles = 0;
         if (b0 + lane < a.B) {
-            const Sequence s = sequence(a, b0 + lane);
-            n = s.nq ? runs_of(tiles_of(s), run) * blocks_of<RB>(a, s) * a.heads : 0;
+            s = sequence(a, b0 + lane);
+            segments = blocks_of<F::rows>(a, s) * a.heads;
+            tiles = segments ? positions_of<F>(s) : 0;
         }
-        const int upto = wave_sum_scan(n);
-        const unsigned long long past = __ballot(before + upto > id);
+        all += segments * tiles;
+        longest = max(longest, tiles);
+    }
+    const bool whole = !a.ws || !__any(longest > kBegin + kWhole);
+    const int W = __builtin_amdgcn_readlane(prefix_sum(all), 63);
+    at.range = whole ? 0 : max(kMinRange, (W + a.target - 1) / a.target);
+    if (!whole && id >= a.target) return false;
+    const int pos = whole ? id : id * at.range;
+    at.first = at.before = 0;
+    for (int b0 = 0;; b0 += 64) {
+        if (a.B > 64) {
+            if (b0 >= a.B) return false;
+            segments = tiles = 0;
+            if (b0 + lane < a.B) {
+                s = sequence(a, b0 + lane);
+                segments = blocks_of<F::rows>(a, s) * a.heads;
+                tiles = segments ? positions_of<F>(s) : 0;
+            }
+        }
+        const int mine = whole ? segments : segments * tiles;
+        const int upto = prefix_sum(mine), segments_upto = prefix_sum(segments);
+        const unsigned long long past = __ballot(at.first + upto > pos);
         if (past) {
-            const int l = __ffsll(past) - 1;
-            b = b0 + l;
-            first = before + __shfl(upto, l) - __shfl(n, l);
+            const int l = __builtin_ctzll(past);
+            at.b = b0 + l;
+            at.before += __builtin_amdgcn_readlane(segments_upto, l) - __builtin_amdgcn_readlane(segments, l);
+            at.first += __builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(mine, l);
+            at.total = whole ? pos + 1 : W;
+            at.s = {__builtin_amdgcn_readlane(s.len, l), __builtin_amdgcn_readlane(s.q0, l), __builtin_amdgcn_readlane(s.nq, l)};
             return true;
         }
-        before += __shfl(upto, 63);
+        if (a.B <= 64) return false;
+        at.first += __builtin_amdgcn_readlane(upto, 63);
+        at.before += __builtin_amdgcn_readlane(segments_upto, 63);
     }
-    return false;
-}
-
-// Of sequence b alone: the id of its first item.
-template <int RB>
-__device__ __forceinline__ long long first_item(const AttnArgs& a, int run, int b) {
-    const int lane = threadIdx.x & 63;
-    long long n = 0;
-    for (int i = lane; i < b; i += 64) {
-        const Sequence s = sequence(a, i);
-        n += s.nq ? runs_of(tiles_of(s), run) * blocks_of<RB>(a, s) * a.heads : 0;
-    }
-#pragma unroll
-    for (int d = 32; d; d /= 2) n += __shfl_xor(n, d);
-    return n;
 }
 
 // Keys that row `row` of a sequence sees: those below the result.
@@ -152,30 +166,24 @@ struct Raw {
 // Indices that the launch only reads, through the scalar cache.
 typedef const int __attribute__((address_space(4))) * const_ints;
 
-template <int D, int NT, int NW, bool BF>
-__global__ __launch_bounds__(64 * NW, NW / 4 * (NT == 1 ? 4 : NT == 2 ? 2 : 1)) void attn_kernel(AttnArgs a) {
-    constexpr int RB = 16 * NT, KS = D / 32, CT = D / 16, W = D / 32;
-    __shared__ float joined[NW / 2][CT * NT][64 * 4];
-    __shared__ float stats[NW][RB][2];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quad = lane >> 4;
+template <int D, int NT, int NW>
+struct Shared {
+    float joined[NW][16 * NT][D + 4], stats[NW][16 * NT][2];
+};
 
-    const int run = __builtin_amdgcn_readfirstlane(plan<RB>(a));
-    int b = 0;
-    long long first = 0;
-    const long long id = blockIdx.x;
-    if (!find_item<RB>(a, run, id, b, first)) return;
-    b = __builtin_amdgcn_readfirstlane(b);
-    const Sequence s = shared_sequence(a, b);
-    const int rbs = blocks_of<RB>(a, s);
-    int rest = __builtin_amdgcn_readfirstlane((int)(id - first));
-    const int h = rest % a.heads;
-    rest /= a.heads;
-    const int rb = rest % rbs, r = rest / rbs;
-    const int rows = s.nq * a.group, row0 = rb * RB;
-    const int most = keys_of(a, s, min(row0 + RB, rows) - 1), least = keys_of(a, s, row0);  // over the block's rows
-    const int tiles = (most + kTile - 1) / kTile, runs = runs_of(tiles, run);
-    if (r >= runs) return;  // these rows see fewer keys than the sequence has
-    const int t0 = r * run, t1 = min(tiles, t0 + run);
+// Tiles t0 .. t1 - 1 of one segment: row block rb and head h of sequence b.  `pieces` workgroups have a part of it, and this one's goes
+// to `slot` if there are several.
+template <int D, int NT, int NW, bool BF>
+__device__ __forceinline__ void segment(const AttnArgs& a, const Sequence& s, int b, int h, int rb, int t0, int t1, int most, int pieces, int slot,
+                                        Shared<D, NT, NW>& lds) {
+    constexpr int RB = 16 * NT, KS = D / 32, CT = D / 16, W = D / 32;
+    auto& joined = lds.joined;
+    auto& stats = lds.stats;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const unsigned col = lane & 15, quad = lane >> 4;
+    const int rows = s.nq * a.group, row0 = rb * RB, least = keys_of(a, s, row0);
+    const bool first = t0 == 0;
+    if (most == 0) t1 = 0;
 
     const const_ints table = (const_ints)(uintptr_t)(a.tables + (long long)b * a.width);
     const int groups_page = 1 << (a.page_shift - 4);
@@ -186,18 +194,21 @@ __global__ __launch_bounds__(64 * NW, NW / 4 * (NT == 1 ? 4 : NT == 2 ? 2 : 1)) 
         const int p = (unsigned)page < (unsigned)a.pages ? page : 0;
         return a.cache + (((long long)p * a.heads + h) * groups_page + (min(g, last_group) & (groups_page - 1))) * Group<D>::bytes;
     };
+    // A lane's places in a group, unsigned so that they are 32-bit offsets to a scalar address.
+    const unsigned k_off = col * (D / 2) + quad * (D / 8), ks_off = Group<D>::k_scales + col * (D / 32) + quad * (D / 4) / 32;
+    const unsigned v_off = Group<D>::v_codes + quad * (2 * D) + col * (D / 8), vs_off = Group<D>::v_scales + quad * (D / 8) + col * (D / 16) / 32 * 4;
     Raw<D> raw;
     auto fetch_k = [&](const uint8_t* at, int i) {
-        const unsigned* k = (const unsigned*)(at + col * (D / 2) + quad * (D / 8));
+        const unsigned* k = (const unsigned*)(at + k_off);
 #pragma unroll
         for (int w = 0; w < W; ++w) raw.k[i][w] = k[w];
-        raw.ks[i] = at[Group<D>::k_scales + col * (D / 32) + quad * (D / 4) / 32];
+        raw.ks[i] = at[ks_off];
     };
     auto fetch_v = [&](const uint8_t* at, int i) {
-        const unsigned* v = (const unsigned*)(at + Group<D>::v_codes + quad * (2 * D) + col * (D / 8));
+        const unsigned* v = (const unsigned*)(at + v_off);
 #pragma unroll
         for (int w = 0; w < W; ++w) raw.v[i][w] = v[w];
-        raw.vs[i] = *(const unsigned*)(at + Group<D>::v_scales + quad * (D / 8) + col * (D / 16) / 32 * 4);
+        raw.vs[i] = *(const unsigned*)(at + vs_off);
     };
     // The first tile's bytes, and the pages of the second, are under way before the queries are asked for.
     int t = t0 + wave, pages[2] = {-1, -1}, ahead[2] = {-1, -1};
@@ -217,7 +228,9 @@ __global__ __launch_bounds__(64 * NW, NW / 4 * (NT == 1 ? 4 : NT == 2 ? 2 : 1)) 
         const bool there = row < rows;
         limit[n] = there ? keys_of(a, s, row) : 0;
         const long long at = ((long long)(s.q0 + (there ? row / a.group : 0)) * a.H + h * a.group + (there ? row % a.group : 0)) * D + quad * (D / 4);
-        factor[n] = a.scale_l2;
+        factor[n] = fabsf(a.scale_l2);  // its sign goes to the queries, and zero too: the largest score is found before this factor
+        const float turn = a.scale_l2 < 0 ? -1.f : a.scale_l2 > 0 ? 1.f : 0.f;
+        if (turn == 0) factor[n] = 1;
         float x[KS][8], top = 0;
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
@@ -236,7 +249,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4 * (NT == 1 ? 4 : NT == 2 ? 2 : 1)) 
 #pragma unroll
         for (int k = 0; k < KS; ++k)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) q[n][k][i] = (_Float16)(BF ? ldexpf(x[k][i], -e) : x[k][i]);
+            for (int i = 0; i < 8; ++i) q[n][k][i] = (_Float16)(turn * (BF ? ldexpf(x[k][i], -e) : x[k][i]));
     }
 
     f32x4 o[NT][CT];
@@ -255,6 +268,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4 * (NT == 1 ? 4 : NT == 2 ? 2 : 1)) 
         float x[NT][8];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
+            if (NT == 1) __builtin_amdgcn_sched_barrier(0);
             f32x4 acc[NT];
 #pragma unroll
             for (int n = 0; n < NT; ++n) acc[n] = {0, 0, 0, 0};
@@ -268,7 +282,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4 * (NT == 1 ? 4 : NT == 2 ? 2 : 1)) 
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) x[n][4 * i + j] = acc[n][j] * factor[n];
+                for (int j = 0; j < 4; ++j) x[n][4 * i + j] = acc[n][j];
         }
         // The next tile's keys take the registers of this one's (behind the run's end: the last group's once more).
         const uint8_t* next[2];
@@ -279,28 +293,43 @@ __global__ __launch_bounds__(64 * NW, NW / 4 * (NT == 1 ? 4 : NT == 2 ? 2 : 1)) 
             ahead[i] = page_of(2 * (t + 2 * NW) + i);
         }
         if (masked) {
+            unsigned nan = 0;
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int i = 0; i < 2; ++i) {
+                // Codes that no row sees are cleared, with their scales: what lies there may be anything.
+                const int key = t * kTile + 16 * i + 4 * quad, live = there[i] ? most - key : 0;  // of the lane's four tokens
+                const unsigned keep = live >= 4 ? ~0u : live <= 0 ? 0u : (1u << (8 * live)) - 1;
+                raw.vs[i] = (raw.vs[i] & keep) | (0x7f7f7f7fu & ~keep);
+                if (D == 128) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int key = t * kTile + 16 * i + 4 * quad + j;
-                    // Values that some row of the block does not see must not reach it as 0 * NaN: a NaN among them goes into the
-                    // scores of the rows that do see it, and the codes that nobody sees are cleared with it.
-                    const unsigned byte = raw.vs[i] << (24 - 8 * j) >> 24;
-                    const unsigned long long bad = __ballot(byte == 255u);
-                    const bool nan = (bad >> (16 * quad) & 0xffffu) != 0;
-                    const bool dead = nan || key >= most || !there[i];
-                    if (dead) {
-                        if (D == 128) raw.v[i][j % W] = 0;
-                        else raw.v[i][j / 2] &= j % 2 ? 0xffffu : 0xffff0000u;
-                        raw.vs[i] = (raw.vs[i] & ~(0xffu << (8 * j))) | 127u << (8 * j);
-                    }
+                    for (int j = 0; j < 4; ++j) raw.v[i][j % W] = j < live ? raw.v[i][j % W] : 0;
+                } else {
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        if (key >= limit[n] || !there[i]) x[n][4 * i + j] = -INFINITY;
-                        else if (nan) x[n][4 * i + j] = __uint_as_float(0x7fc00000u);
-                    }
+                    for (int j = 0; j < 2; ++j) raw.v[i][j] &= (2 * j < live ? 0xffffu : 0u) | (2 * j + 1 < live ? 0xffff0000u : 0u);
                 }
+                nan |= ((raw.vs[i] & 0x7f7f7f7fu) + 0x01010101u) & raw.vs[i] & 0x80808080u;  // bytes of 255
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x[n][4 * i + j] = key + j < limit[n] && there[i] ? x[n][4 * i + j] : -INFINITY;
+            }
+            if (__builtin_expect(__any(nan != 0), 0)) {
+                // A NaN among values that some rows see and others do not must not reach the others as 0 * NaN: it goes into the scores
+                // of the rows that see it.
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const bool mine = (raw.vs[i] >> (8 * j) & 255u) == 255u;
+                        const bool token = (__ballot(mine) >> (16 * quad) & 0xffffu) != 0;
+                        if (mine) raw.vs[i] &= ~(0x80u << (8 * j));
+                        if (D == 128) raw.v[i][j % W] = mine ? 0 : raw.v[i][j % W];
+                        else raw.v[i][j / 2] &= mine ? (j % 2 ? 0xffffu : 0xffff0000u) : ~0u;
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+                            if (token && t * kTile + 16 * i + 4 * quad + j < limit[n]) x[n][4 * i + j] = __uint_as_float(0x7fc00000u);
+                    }
+            }
         }
         f16x8 p[NT];
 #pragma unroll
@@ -308,6 +337,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4 * (NT == 1 ? 4 : NT == 2 ? 2 : 1)) 
             float top = x[n][0];
 #pragma unroll
             for (int j = 1; j < 8; ++j) top = fmaxf(top, x[n][j]);
+            top *= factor[n];
             if (__any(top > m[n] + kRaise)) {  // all four lanes of a row take the same reference
                 top = fmaxf(top, __shfl_xor(top, 16));
                 top = fmaxf(top, __shfl_xor(top, 32));
@@ -321,7 +351,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4 * (NT == 1 ? 4 : NT == 2 ? 2 : 1)) 
             const float ref = m[n] == -INFINITY ? 0.f : m[n];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float e = __builtin_amdgcn_exp2f(x[n][j] - ref);
+                const float e = __builtin_amdgcn_exp2f(fmaf(x[n][j], factor[n], -ref));
                 l[n] += e;
                 p[n][j] = (_Float16)e;
             }
@@ -368,108 +398,417 @@ __global__ __launch_bounds__(64 * NW, NW / 4 * (NT == 1 ? 4 : NT == 2 ? 2 : 1)) 
         for (int i = 0; i < 2; ++i) fetch_v(next[i], i);
     }
 
-    // The waves meet: a common reference for each row, then the upper half's outputs go to the lower half, until one is left.
+    // The waves meet in LDS, all of them once: [wave][row][channel], rows 4 words apart in the banks.  Then a thread has two channels of a
+    // row and adds the waves' in their order.  (Outputs handed on from half of the waves to the other half until one is left took 16 waves 6 us.)
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         l[n] += __shfl_xor(l[n], 16);
         l[n] += __shfl_xor(l[n], 32);
         if (quad == 0) stats[wave][16 * n + col][0] = m[n], stats[wave][16 * n + col][1] = l[n];
+        float* to = joined[wave][16 * n + col] + 4 * quad * CT;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int c = 0; c < CT; c += 4) *(f32x4*)(to + j * CT + c) = f32x4{o[n][c][j], o[n][c + 1][j], o[n][c + 2][j], o[n][c + 3][j]};
     }
     __syncthreads();
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        float top = -INFINITY, sum = 0;
-#pragma unroll
-        for (int w = 0; w < NW; ++w) top = fmaxf(top, stats[w][16 * n + col][0]);
+    for (int i = threadIdx.x; i < RB * (D / 2); i += 64 * NW) {
+        const int at = i / (D / 2), c = 2 * (i % (D / 2)), row = row0 + at;
+        if (row >= rows) break;
+        float top = -INFINITY, sum = 0, x = 0, y = 0;
+#pragma unroll 4
+        for (int w = 0; w < NW; ++w) top = fmaxf(top, stats[w][at][0]);
         const float ref = top == -INFINITY ? 0.f : top;
-#pragma unroll
-        for (int w = 0; w < NW; ++w) sum += stats[w][16 * n + col][1] * __builtin_amdgcn_exp2f(stats[w][16 * n + col][0] - ref);
-        const float by = __builtin_amdgcn_exp2f(m[n] - ref);
-        m[n] = top, l[n] = sum;
-#pragma unroll
-        for (int c = 0; c < CT; ++c) o[n][c] *= by;
-    }
-#pragma unroll
-    for (int half = NW / 2; half; half /= 2) {
-        if (wave >= half && wave < 2 * half)
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int c = 0; c < CT; ++c) *(f32x4*)&joined[wave - half][n * CT + c][4 * lane] = o[n][c];
-        __syncthreads();
-        if (wave < half)
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int c = 0; c < CT; ++c) o[n][c] += *(const f32x4*)&joined[wave][n * CT + c][4 * lane];
-        if (half > 1) __syncthreads();
-    }
-    if (wave) return;
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int row = row0 + 16 * n + col;
-        if (row >= rows) continue;
-        if (runs == 1) {
-            const float by = l[n] == 0.f ? 0.f : 1.f / l[n];
-            const long long vec = (long long)(s.q0 + row / a.group) * a.H + h * a.group + row % a.group;
-            if (quad == 0) a.lse[vec] = l[n] == 0.f ? -INFINITY : (m[n] + __builtin_amdgcn_logf(l[n])) * 0.6931471805599453f;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                unsigned w[CT / 2];
-#pragma unroll
-                for (int c = 0; c < CT / 2; ++c) w[c] = pack2<BF>(o[n][2 * c][j] * by, o[n][2 * c + 1][j] * by);
-                unsigned* to = (unsigned*)(a.out + vec * D + (4 * quad + j) * CT);
-#pragma unroll
-                for (int c = 0; c < CT / 2; ++c) to[c] = w[c];
-            }
+#pragma unroll 4
+        for (int w = 0; w < NW; ++w) {
+            const float by = __builtin_amdgcn_exp2f(stats[w][at][0] - ref);
+            sum += stats[w][at][1] * by;
+            x += joined[w][at][c] * by;
+            y += joined[w][at][c + 1] * by;
+        }
+        const long long vec = (long long)(s.q0 + row / a.group) * a.H + h * a.group + row % a.group;
+        if (a.ws && c == 0 && first) a.heads_ws[vec] = int2{slot * RB + at, pieces};
+        if (pieces == 1) {
+            const float by = sum == 0.f ? 0.f : 1.f / sum;
+            if (c == 0) a.lse[vec] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+            *(unsigned*)(a.out + vec * D + c) = pack2<BF>(x * by, y * by);
         } else {
-            float* to = a.ws + ((id * RB) + 16 * n + col) * (D + 2);
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int c = 0; c < CT; ++c) to[(4 * quad + j) * CT + c] = o[n][c][j];
-            if (quad == 0) to[D] = m[n], to[D + 1] = l[n];
+            float* to = a.ws + (long long)(slot * RB + at) * (D + 2);
+            to[c] = x, to[c + 1] = y;
+            if (c == 0) to[D] = top, to[D + 1] = sum;
         }
     }
 }
 
-// WAVES waves join the runs of one row (query, head): a lane has one run's maximum and sum, then the weighted outputs are added, eight runs'
-// loads at a time (one run after another took 75 us for rows of 128 runs).
+// Many rows: a wave has 32 rows, all waves go over the same tiles of 64 keys, and the converted tile lies in LDS, in the order in which
+// the 32 x 32 x 16 MFMA takes its first operand, so that 16 bytes of a lane are one read.  A tile is converted once for the workgroup's
+// rows, one ahead of its use, from bytes that were asked for another one ahead.
+//     S^T (32 tokens x 32 rows) = K Q^T:  lane l has row l % 32 of Q, register v token 8 (v / 4) + 4 (l / 32) + v % 4
+//     O^T (32 channels x 32 rows) += V^T P^T: P as S^T leaves it, so half l / 32 has tokens 4 (l / 32) .. + 3 and 8 + 4 (l / 32) .. + 3 of 16
+// A row's output stays in one wave: nothing to join within the workgroup.
+constexpr int kWideTile = 64;
+
+template <int D>
+struct WideShared {
+    uint4 k[2][2 * (D / 16) * 64], v[2][4 * (D / 32) * 64];  // [buffer][32 tokens][16 channels][lane], [buffer][16 tokens][32 channels][lane]
+    unsigned flags[2][4];  // of 16 tokens: whose values hold a NaN, and (bit 16) whether their page is outside the cache
+};
+
+template <int D, int NW, bool BF>
+__device__ __forceinline__ void wide_segment(const AttnArgs& a, const Sequence& s, int b, int h, int rb, int t0, int t1, int most, int pieces,
+                                             int slot, WideShared<D>& lds) {
+    constexpr int RB = 32 * NW, KS = D / 16, CT = D / 32, W = D / 32, RUN = D / 16;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const unsigned col = lane & 31, half = lane >> 5, c16 = lane & 15, quad = lane >> 4;
+    const int rows = s.nq * a.group, row0 = rb * RB + 32 * wave, row = row0 + (int)col;
+    const bool first = t0 == 0, mine = row < rows;
+    if (most == 0) t1 = 0;
+    // The wave's own rows: keys that its first row sees, and its last one.
+    const int least = row0 < rows ? keys_of(a, s, row0) : 0, top_key = row0 < rows ? keys_of(a, s, min(row0 + 32, rows) - 1) : 0;
+    const int limit = mine ? keys_of(a, s, row) : 0;
+
+    const const_ints table = (const_ints)(uintptr_t)(a.tables + (long long)b * a.width);
+    const int groups_page = 1 << (a.page_shift - 4), last_group = max(0, (most + 15) / 16 - 1);
+    auto page_of = [&](int g) { return table[min(g, last_group) >> (a.page_shift - 4)]; };
+    auto group_at = [&](int g, int page) {
+        const int p = (unsigned)page < (unsigned)a.pages ? page : 0;
+        return a.cache + (((long long)p * a.heads + h) * groups_page + (min(g, last_group) & (groups_page - 1))) * Group<D>::bytes;
+    };
+    // Groups of 16 tokens are shared out: with eight waves four convert keys and four values, with four a wave does both of its group.
+    const int mine_g = wave & 3;
+    const bool keys = NW == 4 || wave < 4, vals = NW == 4 || wave >= 4;
+    unsigned rk[W], rv[W], rks = 0, rvs = 0;
+    const unsigned k_off = c16 * (D / 2) + quad * (D / 8), ks_off = Group<D>::k_scales + c16 * (D / 32) + quad * (D / 4) / 32;
+    const unsigned v_off = Group<D>::v_codes + quad * (2 * D) + c16 * (D / 8), vs_off = Group<D>::v_scales + quad * (D / 8) + c16 * (D / 16) / 32 * 4;
+    auto fetch = [&](const uint8_t* at) {
+        if (keys) {
+            const unsigned* k = (const unsigned*)(at + k_off);
+#pragma unroll
+            for (int w = 0; w < W; ++w) rk[w] = k[w];
+            rks = at[ks_off];
+        }
+        if (vals) {
+            const unsigned* v = (const unsigned*)(at + v_off);
+#pragma unroll
+            for (int w = 0; w < W; ++w) rv[w] = v[w];
+            rvs = *(const unsigned*)(at + vs_off);
+        }
+    };
+    auto put = [&](int t, int page) {
+        const int buf = t & 1;
+        if (keys) {  // the lane's token and D/4 channels from quad * D/4
+            uint4* to = lds.k[buf] + ((mine_g >> 1) * KS * 64 + (mine_g & 1) * 16 + c16);
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                const unsigned piece = quad * W + w;  // 8 channels: half piece % 2 of 16
+                to[(piece >> 1) * 64 + (piece & 1) * 32] = values8<false>(rk[w], rks << 23);
+            }
+        }
+        if (vals) {
+            const int key = t * kWideTile + 16 * mine_g + 4 * (int)quad;
+            const bool there = (unsigned)page < (unsigned)a.pages;
+            if (!there || t * kWideTile + 16 * mine_g + 16 > most) {
+                const int live = there ? most - key : 0;
+                const unsigned keep = live >= 4 ? ~0u : live <= 0 ? 0u : (1u << (8 * live)) - 1;
+                rvs = (rvs & keep) | (0x7f7f7f7fu & ~keep);
+#pragma unroll
+                for (int w = 0; w < W; ++w)
+                    rv[w] = D == 128 ? (w < live ? rv[w] : 0) : rv[w] & ((2 * w < live ? 0xffffu : 0u) | (2 * w + 1 < live ? 0xffff0000u : 0u));
+            }
+            // A NaN must reach the rows that see its token and no other: it goes into their scores, and its codes are cleared.
+            unsigned flags = there ? 0 : 1u << 16;
+            if (__builtin_expect(__any((((rvs & 0x7f7f7f7fu) + 0x01010101u) & rvs & 0x80808080u) != 0), 0)) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const bool bad = (rvs >> (8 * j) & 255u) == 255u;
+                    const unsigned long long all = __ballot(bad);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        if (all >> (16 * q) & 0xffffu) flags |= 1u << (4 * q + j);
+                    if (bad) rvs &= ~(0x80u << (8 * j));
+                    if (D == 128) rv[j % W] = bad ? 0 : rv[j % W];
+                    else rv[j / 2] &= bad ? (j % 2 ? 0xffffu : 0xffff0000u) : ~0u;
+                }
+            }
+            if (lane == 0) lds.flags[buf][mine_g] = flags;
+            const unsigned sc[4] = {rvs << 23, rvs << 15, rvs << 7, rvs >> 1};
+            // Four tokens of a channel are 8 bytes: half quad % 2, the lower or upper 8 bytes of the lane's 16 by quad / 2.
+            uint2* to = (uint2*)lds.v[buf] + (mine_g * CT * 64 + (quad & 1) * 32 + c16) * 2 + (quad >> 1);
+            auto channels = [&](auto SEL) {
+                constexpr int c = decltype(SEL)::value;
+                unsigned two[4];
+                if constexpr (D == 128) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) two[j] = values2<false, c>(rv[j % W], sc[j]);
+                } else {
+                    two[0] = values2<false, c>(rv[0], sc[0]), two[1] = values2<false, 2 + c>(rv[0], sc[1]);
+                    two[2] = values2<false, c>(rv[1], sc[2]), two[3] = values2<false, 2 + c>(rv[1], sc[3]);
+                }
+                to[c * 128] = uint2{__builtin_amdgcn_perm(two[1], two[0], 0x05040100u), __builtin_amdgcn_perm(two[3], two[2], 0x05040100u)};
+                to[c * 128 + 32] = uint2{__builtin_amdgcn_perm(two[1], two[0], 0x07060302u), __builtin_amdgcn_perm(two[3], two[2], 0x07060302u)};
+            };
+            channels(std::integral_constant<int, 0>());
+            channels(std::integral_constant<int, 1>());
+            if constexpr (D == 128) {
+                channels(std::integral_constant<int, 2>());
+                channels(std::integral_constant<int, 3>());
+            }
+        }
+    };
+
+    int page = -1, ahead = -1;
+    if (t0 < t1) {
+        page = page_of(4 * t0 + mine_g);
+        ahead = page_of(4 * (t0 + 1) + mine_g);
+        fetch(group_at(4 * t0 + mine_g, page));
+    }
+
+    // Queries: the lane's row, channels 16 ks + 8 half .. + 7.
+    f16x8 q[KS];
+    float factor = fabsf(a.scale_l2);  // as in `segment`
+    {
+        const float turn = a.scale_l2 < 0 ? -1.f : a.scale_l2 > 0 ? 1.f : 0.f;
+        if (turn == 0) factor = 1;
+        const long long at = ((long long)(s.q0 + (mine ? row / a.group : 0)) * a.H + h * a.group + (mine ? row % a.group : 0)) * D + 8 * half;
+        float top = 0;
+        uint4 raw[KS];
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+            raw[k] = *(const uint4*)(a.q + at + 16 * k);
+            float x[8];
+            values_of<BF>(raw[k], x);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[i]));
+        }
+        int e = 0;
+        if (BF) {
+            top = fmaxf(top, __shfl_xor(top, 32));
+            if (top > 0 && top < INFINITY) e = ilogbf(top);
+            factor *= ldexpf(1.f, e);
+        }
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+            float x[8];
+            values_of<BF>(raw[k], x);
+            if (k == 0 && top == INFINITY) x[0] = __uint_as_float(0x7fc00000u);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) q[k][i] = (_Float16)(turn * (BF ? ldexpf(x[i], -e) : x[i]));
+        }
+    }
+    f32x16 o[CT];
+#pragma unroll
+    for (int c = 0; c < CT; ++c)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) o[c][v] = 0;
+    float m = -INFINITY, l = 0;
+
+    if (t0 < t1) {
+        put(t0, page);
+        page = ahead;
+        fetch(group_at(4 * (t0 + 1) + mine_g, page));
+        ahead = page_of(4 * (t0 + 2) + mine_g);
+    }
+    for (int t = t0; t < t1; ++t) {
+        __syncthreads();  // tile t is there, and nobody reads the other buffer any more
+        const int buf = t & 1;
+        const bool work = t * kWideTile < top_key;
+        f32x16 x[2];
+        if (work) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+#pragma unroll
+                for (int v = 0; v < 16; ++v) x[i][v] = 0;
+#pragma unroll
+                for (int k = 0; k < KS; ++k)
+                    x[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, lds.k[buf][(i * KS + k) * 64 + lane]), q[k], x[i], 0, 0, 0);
+            }
+        }
+        if (t + 1 < t1) {
+            put(t + 1, page);
+            page = ahead;
+            fetch(group_at(4 * (t + 2) + mine_g, page));
+            ahead = page_of(4 * (t + 3) + mine_g);
+        }
+        if (!work) continue;
+        const uint4 flags = *(const uint4*)lds.flags[buf];
+        const unsigned any = __builtin_amdgcn_readfirstlane(flags.x | flags.y | flags.z | flags.w);
+        if ((t + 1) * kWideTile > least || any) {
+            const unsigned f[4] = {flags.x, flags.y, flags.z, flags.w};
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    const int in = 8 * (v / 4) + v % 4;  // token of the 32, less 4 half
+                    const int key = t * kWideTile + 32 * i + in + 4 * (int)half;
+                    x[i][v] = key < limit ? x[i][v] : -INFINITY;
+                    if (any) {
+                        const unsigned g = f[2 * i + in / 16];
+                        if (g >> 16) x[i][v] = -INFINITY;
+                        else if (g >> (in % 16 + 4 * half) & 1 && key < limit) x[i][v] = __uint_as_float(0x7fc00000u);
+                    }
+                }
+        }
+        float top = x[0][0];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) top = fmaxf(top, x[i][v]);
+        top *= factor;
+        if (__any(top > m + kRaise)) {
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float to = fmaxf(m, top);
+            const float by = to == m ? 1.f : __builtin_amdgcn_exp2f(m - to);
+            m = to;
+            l *= by;
+#pragma unroll
+            for (int c = 0; c < CT; ++c) o[c] *= by;
+        }
+        const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                f16x8 p;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float e = __builtin_amdgcn_exp2f(fmaf(x[i][8 * k + j], factor, -ref));
+                    l += e;
+                    p[j] = (_Float16)e;
+                }
+#pragma unroll
+                for (int c = 0; c < CT; ++c)
+                    o[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, lds.v[buf][((2 * i + k) * CT + c) * 64 + lane]), p, o[c], 0, 0, 0);
+            }
+    }
+
+    l += __shfl_xor(l, 32);
+    if (!mine) return;
+    const long long vec = (long long)(s.q0 + row / a.group) * a.H + h * a.group + row % a.group;
+    const int at = slot * RB + 32 * wave + (int)col;
+    if (a.ws && half == 0 && first) a.heads_ws[vec] = int2{at, pieces};
+    const float by = l == 0.f ? 0.f : 1.f / l;
+    if (half == 0) {
+        if (pieces == 1) a.lse[vec] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+        else a.ws[(long long)at * (D + 2) + D] = m, a.ws[(long long)at * (D + 2) + D + 1] = l;
+    }
+    // Row 16 i + r of channel tile c is channel 2 c + i of run r: a lane has all channels of its runs.
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int channel = (8 * u + 4 * (int)half + r) * RUN;
+            if (pieces == 1) {
+                unsigned w[CT];
+#pragma unroll
+                for (int c = 0; c < CT; ++c) w[c] = pack2<BF>(o[c][4 * u + r] * by, o[c][8 + 4 * u + r] * by);
+                unsigned* to = (unsigned*)(a.out + vec * D + channel);
+#pragma unroll
+                for (int c = 0; c < CT; ++c) to[c] = w[c];
+            } else {
+                float* to = a.ws + (long long)at * (D + 2) + channel;
+#pragma unroll
+                for (int c = 0; c < CT; ++c) to[2 * c] = o[c][4 * u + r], to[2 * c + 1] = o[c][8 + 4 * u + r];
+            }
+        }
+}
+
+// The two forms of a segment: NT tiles of 16 rows with the keys shared out to NW waves, or 32 rows to each of NW waves.
+template <int D, int NT, int NW, bool BF>
+struct Narrow {
+    static constexpr int rows = 16 * NT, tile = kTile, waves_simd = NT == 1 ? 4 : NT == 2 ? 2 : 1, threads = 64 * NW;
+    typedef Shared<D, NT, NW> Lds;
+    template <class... A>
+    static __device__ __forceinline__ void run(A&&... x) { segment<D, NT, NW, BF>(x...); }
+};
+template <int D, int NW, bool BF>
+struct Wide {
+    static constexpr int rows = 32 * NW, tile = kWideTile, waves_simd = 2, threads = 64 * NW;
+    typedef WideShared<D> Lds;
+    template <class... A>
+    static __device__ __forceinline__ void run(A&&... x) { wide_segment<D, NW, BF>(x...); }
+};
+
+template <class F>
+__global__ __launch_bounds__(F::threads, F::waves_simd) void attn_kernel(AttnArgs a) {
+    constexpr int RB = F::rows;
+    __shared__ typename F::Lds lds;
+    const int id = blockIdx.x;
+    Start at;
+    if (!start_of<F>(a, id, at)) return;
+    Sequence s = at.s;
+    int b = at.b, of = positions_of<F>(s), segments = blocks_of<RB>(a, s) * a.heads;
+    int seg = id - at.first, w0 = 0, left = of;  // a whole segment
+    if (at.range) {
+        const int pos = id * at.range;
+        seg = (pos - at.first) / of;
+        w0 = pos - at.first - seg * of;
+        left = min(at.range, at.total - pos);
+    }
+    for (;;) {
+        const int w1 = min(of, w0 + left), rb = seg / a.heads;
+        // The keys that the row block's last row sees may be fewer than the sequence has.
+        const int most = keys_of(a, s, min((rb + 1) * RB, s.nq * a.group) - 1), tiles = max(1, (most + F::tile - 1) / F::tile);
+        int pieces = 1;
+        if (at.range) {
+            const int from = at.first + seg * of + kBegin;
+            pieces = (from + tiles - 1) / at.range - from / at.range + 1;
+        }
+        const int t0 = max(0, w0 - kBegin), t1 = min(tiles, w1 - kBegin);
+        if (t0 < t1) F::run(a, s, b, seg % a.heads, rb, t0, t1, most, pieces, id + at.before + seg, lds);
+        left -= w1 - w0;
+        if (left <= 0) return;
+        __syncthreads();  // the next segment takes this one's place in LDS
+        w0 = 0;
+        if (++seg < segments) continue;
+        at.first += segments * of, at.before += segments, seg = 0;
+        do {  // positions are left, so a sequence with rows is
+            s = shared_sequence(a, ++b);
+            segments = blocks_of<RB>(a, s) * a.heads;
+        } while (!segments);
+        of = positions_of<F>(s);
+    }
+}
+
+// WAVES waves join the pieces of one row (query, head): a lane has one piece's maximum and sum, then the weighted outputs are added, eight pieces'
+// loads at a time (one after another took 75 us for rows of 128).
 template <int D, int RB, bool BF, int WAVES>
-__global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
-    constexpr int C = D / 64;
-    __shared__ float part[WAVES > 1 ? 4 : 1][D + 2];
+__global__ __launch_bounds__(WAVES > 4 ? 64 * WAVES : 256) void join_kernel(AttnArgs a) {
+    constexpr int C = D / 64, ROWS = WAVES > 4 ? 1 : 4 / WAVES;  // of a workgroup
+    __shared__ float part[WAVES][D + 2];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), mine = wave % WAVES;
-    const long long vec = (long long)blockIdx.x * (4 / WAVES) + wave / WAVES;
+    const long long vec = (long long)blockIdx.x * ROWS + wave / WAVES;
     if (vec >= (long long)a.T * a.H) return;
-    const int t = (int)(vec / a.H), head = (int)(vec % a.H), h = head / a.group;
-    int b;
-    if (a.cu_q) {  // the sequence with cu_q[b] <= t < cu_q[b + 1]
+    const int t = (int)(vec / a.H);
+    const int2 mine_at = a.heads_ws[vec];  // for a row of nobody: anything
+    if (a.cu_q) {
         int upto = 0;
         for (int i = lane; i < a.B; i += 64) upto += a.cu_q[i + 1] <= t;
 #pragma unroll
         for (int d = 32; d; d /= 2) upto += __shfl_xor(upto, d);
-        b = __builtin_amdgcn_readfirstlane(upto);
-        if (b >= a.B || t < a.cu_q[b]) return;
-    } else {
-        b = t / a.max_q;
+        const int b = __builtin_amdgcn_readfirstlane(upto);
+        if (b >= a.B) return;
+        const Sequence s = shared_sequence(a, b);
+        if (t < s.q0 || t - s.q0 >= s.nq) return;
     }
-    const int run = __builtin_amdgcn_readfirstlane(plan<RB>(a));
-    const Sequence s = shared_sequence(a, b);
-    if (t - s.q0 >= s.nq) return;
-    const int row = (t - s.q0) * a.group + head % a.group, rb = row / RB, rows = s.nq * a.group;
-    const int most = keys_of(a, s, min((rb + 1) * RB, rows) - 1);
-    const int runs = runs_of((most + kTile - 1) / kTile, run);
+    const int runs = __builtin_amdgcn_readfirstlane(mine_at.y);
     if (runs == 1) return;
-    const int rbs = blocks_of<RB>(a, s);
-    const long long id = first_item<RB>(a, run, b) + (long long)rb * a.heads + h, step = (long long)rbs * a.heads * RB * (D + 2);
-    const float* from = a.ws + (id * RB + row % RB) * (D + 2);
-    // Lane l has run r0 + WAVES l: its reference is raised for 64 runs at a time.
+    const float* from = a.ws + (long long)__builtin_amdgcn_readfirstlane(mine_at.x) * (D + 2);
+    constexpr long long step = RB * (D + 2);
+    // Lane l has piece r0 + WAVES l: its reference is raised for 64 pieces at a time.
     float top = -INFINITY, sum = 0, o[C] = {};
     for (int r0 = mine; r0 < runs; r0 += 64 * WAVES) {
         const int r = r0 + WAVES * lane;
         float m = -INFINITY, l = 0;
         if (r < runs) m = from[r * step + D], l = from[r * step + D + 1];
+        const int n = min(64, (runs - r0 + WAVES - 1) / WAVES);
+        float x[8][C];
+        auto fetch = [&](int k) {
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+#pragma unroll
+                for (int i = 0; i < C; ++i) x[u][i] = from[(r0 + WAVES * min(k + u, n - 1)) * step + lane * C + i];
+        };
+        fetch(0);  // under way together with the maxima
         float to = m;
 #pragma unroll
         for (int d = 32; d; d /= 2) to = fmaxf(to, __shfl_xor(to, d));
@@ -477,15 +816,10 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
         const float ref = to == -INFINITY ? 0.f : to, by = __builtin_amdgcn_exp2f(top - ref);
         const float weight = __builtin_amdgcn_exp2f(m - ref);
         top = to;
-        sum = sum * by + weight * l;  // each lane's own runs
+        sum = sum * by + weight * l;  // each lane's own pieces
         for (int i = 0; i < C; ++i) o[i] *= by;
-        const int n = min(64, (runs - r0 + WAVES - 1) / WAVES);
         for (int k = 0; k < n; k += 8) {
-            float x[8][C];
-#pragma unroll
-            for (int u = 0; u < 8; ++u)
-#pragma unroll
-                for (int i = 0; i < C; ++i) x[u][i] = from[(r0 + WAVES * min(k + u, n - 1)) * step + lane * C + i];
+            if (k) fetch(k);
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
                 const float w = __shfl(weight, min(k + u, n - 1));
@@ -523,51 +857,69 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
     }
 }
 
+#ifndef KWW
+#define KWW 8
+#endif
 struct Choice {
-    int nt, nw, target;
-    long long blocks, bytes;
+    int wide, nt, nw, rows, target;  // wide: 32 rows a wave; otherwise nt tiles of 16 rows
+    long long blocks, slots, bytes;
 };
 
 constexpr int kShort = 2048;   // keys
-constexpr int kTarget = 1024;  // runs of a launch: four workgroups on each of 256 units
+constexpr int kRanges = 1024;  // four workgroups of 128 registers on each of 256 units
 
-Choice choose(int B, int heads, int group, int d, long long cap, int max_q) {
-    const long long rows = (long long)group * max_q;
+Choice choose(long long T, int B, int H, int heads, int d, long long cap, int max_q) {
+    const long long rows = (long long)(H / heads) * max_q;
     Choice c;
+    c.wide = rows > 64;
     c.nt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-    c.target = kTarget;
-    const long long rbs = (rows + 16 * c.nt - 1) / (16 * c.nt), alone = B * rbs * heads;
-    // Sequences that cannot be long are not cut: 16 waves go over up to four tiles each, and there is nothing to join.
-    const bool one = cap <= kShort;
-    c.nw = one && c.nt == 1 ? 16 : 4;
-    c.blocks = one ? alone : alone + c.target;
-    c.bytes = one ? 0 : c.blocks * 16 * c.nt * (d + 2) * 4;
+    c.nw = c.wide ? (rows <= 128 ? 4 : KWW) : 4;
+    c.rows = c.wide ? 32 * c.nw : 16 * c.nt;
+    c.target = c.wide ? 2048 / c.nw : kRanges;
+    const long long alone = B * ((rows + c.rows - 1) / c.rows) * heads;
+    // Segments that fill the launch by themselves stay whole, and so do those that cannot be long: if they are few, 16 waves take one,
+    // up to four tiles each.
+    const bool whole = cap <= kShort || alone >= 4 * c.target;
+    if (c.nt == 1 && cap <= kShort && alone <= 256) c.nw = 16;
+    c.blocks = whole || alone > c.target ? alone : c.target;
+    c.slots = c.target + alone;
+    c.bytes = whole ? 0 : (T * H * 8 + 15) / 16 * 16 + c.slots * c.rows * (d + 2) * 4;
     return c;
 }
 
-int check_sizes(int B, int H, int heads, int d, int page_size, int width, int max_q) {
-    if (B < 1 || heads < 1 || H < heads || H % heads || width < 1 || max_q < 1) return KV4_EINVAL;
+int check_sizes(long long T, int B, int H, int heads, int d, int page_size, int width, int max_q) {
+    if (T < 0 || B < 1 || heads < 1 || H < heads || H % heads || width < 1 || max_q < 1) return KV4_EINVAL;
     if (page_size < 16 || page_size > 65536 || (page_size & (page_size - 1))) return KV4_EINVAL;
     if (d != 64 && d != 128) return KV4_EUNSUPPORTED;
-    if ((long long)width * page_size > INT_MAX || (long long)(H / heads) * max_q > 1 << 30 || B > 65535) return KV4_EUNSUPPORTED;
-    return choose(B, heads, H / heads, d, (long long)width * page_size, max_q).blocks >= 1 << 23 ? KV4_EUNSUPPORTED : KV4_OK;
+    const long long cap = (long long)width * page_size, rows = (long long)(H / heads) * max_q;
+    if (cap > INT_MAX || rows > 1 << 30 || B > 65535 || T * H > INT_MAX) return KV4_EUNSUPPORTED;
+    const Choice c = choose(T, B, H, heads, d, cap, max_q);
+    // Positions and rows of pieces are counted in 32 bits.
+    return c.blocks >= 1 << 23 || (c.bytes && (double)(c.blocks + c.target) * (double)(cap / kTile + kBegin + kMinRange) > INT_MAX) ? KV4_EUNSUPPORTED : KV4_OK;
 }
 
 template <int D, bool BF>
 int launch_attn(const Choice& c, AttnArgs& a, void* stream) {
-    const void* fn = c.nw == 16  ? (const void*)attn_kernel<D, 1, 16, BF>
-                     : c.nt == 1 ? (const void*)attn_kernel<D, 1, 4, BF>
-                     : c.nt == 2 ? (const void*)attn_kernel<D, 2, 4, BF>
-                                 : (const void*)attn_kernel<D, 4, 4, BF>;
-    // Rows enough to fill the units get a wave each, fewer ones a workgroup: those are the rows with many runs.
+    const void* fn = c.wide      ? (c.nw == 8 ? (const void*)attn_kernel<Wide<D, 8, BF>> : (const void*)attn_kernel<Wide<D, 4, BF>>)
+                     : c.nw == 16 ? (const void*)attn_kernel<Narrow<D, 1, 16, BF>>
+                     : c.nt == 1  ? (const void*)attn_kernel<Narrow<D, 1, 4, BF>>
+                     : c.nt == 2  ? (const void*)attn_kernel<Narrow<D, 2, 4, BF>>
+                                  : (const void*)attn_kernel<Narrow<D, 4, 4, BF>>;
+    // Rows enough to fill the units get a wave each, fewer ones four, and the fewest, which have the most pieces, sixteen.
     const long long rows = (long long)a.T * a.H;
-    const bool many = rows >= 4096;
-    const void* join = c.nt == 1   ? (many ? (const void*)join_kernel<D, 16, BF, 1> : (const void*)join_kernel<D, 16, BF, 4>)
-                       : c.nt == 2 ? (many ? (const void*)join_kernel<D, 32, BF, 1> : (const void*)join_kernel<D, 32, BF, 4>)
-                                   : (many ? (const void*)join_kernel<D, 64, BF, 1> : (const void*)join_kernel<D, 64, BF, 4>);
+    const int waves = rows >= 4096 ? 1 : rows >= 512 ? 4 : 16;
+    auto join_of = [&](auto RB) {
+        constexpr int rb = decltype(RB)::value;
+        return waves == 1 ? (const void*)join_kernel<D, rb, BF, 1> : waves == 4 ? (const void*)join_kernel<D, rb, BF, 4> : (const void*)join_kernel<D, rb, BF, 16>;
+    };
+    const void* join = c.rows == 16    ? join_of(std::integral_constant<int, 16>())
+                       : c.rows == 32  ? join_of(std::integral_constant<int, 32>())
+                       : c.rows == 64  ? join_of(std::integral_constant<int, 64>())
+                       : c.rows == 128 ? join_of(std::integral_constant<int, 128>())
+                                       : join_of(std::integral_constant<int, 256>());
     void* list[] = {&a};
     if (hipLaunchKernel(fn, dim3((unsigned)c.blocks), dim3(64 * c.nw), list, 0, (hipStream_t)stream) != hipSuccess ||
-        (a.ws && hipLaunchKernel(join, dim3((unsigned)(many ? (rows + 3) / 4 : rows)), dim3(256), list, 0, (hipStream_t)stream) != hipSuccess)) {
+        (a.ws && hipLaunchKernel(join, dim3((unsigned)(waves == 1 ? (rows + 3) / 4 : rows)), dim3(waves == 16 ? 1024 : 256), list, 0, (hipStream_t)stream) != hipSuccess)) {
         (void)hipGetLastError();
         return KV4_ELAUNCH;
     }
@@ -592,22 +944,23 @@ int kv4_attn(const void* q, const void* cache, const int* tables, const int* len
     if ((dtype != KV4_F16 && dtype != KV4_BF16) || !isfinite(scale)) return KV4_EINVAL;
     if (T == 0 && B >= 1) return KV4_OK;
     if (!cu_q && (B < 1 || T % B || max_q != T / B)) return KV4_EINVAL;
-    if (const int rc = check_sizes(B, H, heads, d, page_size, width, max_q)) return rc;
-    if ((long long)pages * page_size > INT_MAX || (long long)T * H > INT_MAX) return KV4_EUNSUPPORTED;
+    if (const int rc = check_sizes(T, B, H, heads, d, page_size, width, max_q)) return rc;
+    if ((long long)pages * page_size > INT_MAX) return KV4_EUNSUPPORTED;
     const long long bytes = (long long)T * H * d * 2;
     if (overlap(q, bytes, out, bytes) || overlap(lse, (long long)T * H * 4, out, bytes)) return KV4_EINVAL;
-    const Choice c = choose(B, heads, H / heads, d, (long long)width * page_size, max_q);
+    const Choice c = choose(T, B, H, heads, d, (long long)width * page_size, max_q);
     const bool cut = c.bytes && workspace && workspace_bytes >= c.bytes;
-    AttnArgs a = {(const uint16_t*)q, (const uint8_t*)cache, tables, lens, cu_q, (uint16_t*)out, lse, cut ? (float*)workspace : nullptr,
-                  T, B, H, heads, H / heads, pages, __builtin_ctz(page_size), width, max_q, causal, scale * 1.4426950408889634f, c.target};
+    AttnArgs a = {(const uint16_t*)q, (const uint8_t*)cache, tables, lens, cu_q, (uint16_t*)out, lse, cut ? (int2*)workspace : nullptr,
+                  cut ? (float*)((char*)workspace + c.bytes - c.slots * c.rows * (d + 2) * 4) : nullptr, T, B, H,
+                  heads, H / heads, pages, __builtin_ctz(page_size), width, max_q, causal, scale * 1.4426950408889634f, c.target};
     if (d == 128) return dtype ? launch_attn<128, true>(c, a, stream) : launch_attn<128, false>(c, a, stream);
     return dtype ? launch_attn<64, true>(c, a, stream) : launch_attn<64, false>(c, a, stream);
 }
 
-long long kv4_attn_workspace(int B, int H, int heads, int d, int page_size, int width, int max_q) {
+long long kv4_attn_workspace(int T, int B, int H, int heads, int d, int page_size, int width, int max_q) {
     using namespace kv4;
-    if (const int rc = check_sizes(B, H, heads, d, page_size, width, max_q)) return rc;
-    return choose(B, heads, H / heads, d, (long long)width * page_size, max_q).bytes;
+    if (const int rc = check_sizes(T, B, H, heads, d, page_size, width, max_q)) return rc;
+    return choose(T, B, H, heads, d, (long long)width * page_size, max_q).bytes;
 }
 
 }  // extern "C"

@@ -22,8 +22,7 @@ __device__ __forceinline__ unsigned bits_of(T x) {
 
 // Eight 16-bit elements as floats.
 template <bool BF>
-__device__ __forceinline__ void load8(const uint16_t* p, float* x) {
-    const uint4 w = *(const uint4*)p;
+__device__ __forceinline__ void values_of(uint4 w, float* x) {
     const unsigned u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -36,6 +35,11 @@ __device__ __forceinline__ void load8(const uint16_t* p, float* x) {
             x[2 * i + 1] = (float)h[1];
         }
     }
+}
+
+template <bool BF>
+__device__ __forceinline__ void load8(const uint16_t* p, float* x) {
+    values_of<BF>(*(const uint4*)p, x);
 }
 
 __device__ __forceinline__ void load8f(const float* p, float* x) {

@@ -295,7 +295,7 @@ PyObject* cached_attn(PyObject* const* args, Py_ssize_t nargs) {
     const double scale = r.number(args[7]);
     void* stream;
     if (!r.ok || (!cu && max_q != T / B) || !stream_of(args[11], *q, &stream)) return not_plain();
-    const long long need = g_kv4_attn_workspace(B, H, heads, d, page, width, max_q);
+    const long long need = g_kv4_attn_workspace(T, B, H, heads, d, page, width, max_q);
     if (need < 0) return PyLong_FromLong(need);
     void* given = nullptr;
     if (args[10] != Py_None) {

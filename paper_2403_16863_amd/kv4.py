@@ -35,7 +35,7 @@ def lib():
         L.kv4_attn.restype = i
         L.kv4_attn.argtypes = [vp] * 7 + [i] * 10 + [f, i, vp, ll, vp]
         L.kv4_attn_workspace.restype = ll
-        L.kv4_attn_workspace.argtypes = [i] * 7
+        L.kv4_attn_workspace.argtypes = [i] * 8
         L.kv4_strerror.restype = ctypes.c_char_p
         L.kv4_strerror.argtypes = [i]
         _ready = True
@@ -181,9 +181,9 @@ def kv4_read(cache, slots, k=None, v=None, stream=None) -> None:
         raise Kv4Error(rc, "kv4_read")
 
 
-def kv4_attn_workspace(B: int, H: int, heads: int, d: int, page_size: int, width: int, max_q: int) -> int:
+def kv4_attn_workspace(T: int, B: int, H: int, heads: int, d: int, page_size: int, width: int, max_q: int) -> int:
     """Bytes of scratch memory that kv4_attn has a use for (0: none)."""
-    n = lib().kv4_attn_workspace(int(B), int(H), int(heads), int(d), int(page_size), int(width), int(max_q))
+    n = lib().kv4_attn_workspace(int(T), int(B), int(H), int(heads), int(d), int(page_size), int(width), int(max_q))
     if n < 0:
         raise Kv4Error(n, "kv4_attn_workspace")
     return n
@@ -231,7 +231,7 @@ def kv4_attn(q, cache, tables, lens, out, lse, causal: bool, scale: float, cu_q=
     if T == 0:
         return
     st = _stream(stream, cache.device)
-    need = kv4_attn_workspace(B, H, heads, d, page_size, width, max_q)
+    need = kv4_attn_workspace(T, B, H, heads, d, page_size, width, max_q)
     if workspace is not None:
         if not workspace.is_contiguous() or workspace.numel() * workspace.element_size() < need:
             raise ValueError(f"workspace must be contiguous with {need} bytes")

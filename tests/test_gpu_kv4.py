@@ -358,7 +358,7 @@ def test_given_workspace_and_small_ones():
     from paper_2403_16863_amd import kv4
     s = setup(([3000], [1], 8, 2, 128, 16, True), torch.float16)
     B, width = s["tables"].shape
-    need = kv4.kv4_attn_workspace(B, 8, 2, 128, 16, width, 1)
+    need = kv4.kv4_attn_workspace(1, B, 8, 2, 128, 16, width, 1)
     assert need > 0
     want = run(s)
     got = run(s, workspace=torch.full((need,), 255, dtype=torch.uint8, device="cuda"))

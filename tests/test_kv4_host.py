@@ -58,9 +58,9 @@ def test_attention_refuses_bad_arguments():
     for bad in (dict(d=96), dict(width=1 << 28), dict(pages=1 << 28), dict(B=65536), dict(T=1 << 30), dict(max_q=1 << 30)):
         assert call(**bad) == kv4.KV4_EUNSUPPORTED, bad
     assert call(T=0) == kv4.KV4_OK
-    assert L.kv4_attn_workspace(2, 5, 2, 64, 16, 5, 1) == kv4.KV4_EINVAL
-    assert L.kv4_attn_workspace(1, 4, 2, 64, 16, 2, 1) == 0         # no sequence that long is cut
-    assert L.kv4_attn_workspace(1, 4, 2, 64, 16, 500, 1) > 0
+    assert L.kv4_attn_workspace(2, 2, 5, 2, 64, 16, 5, 1) == kv4.KV4_EINVAL
+    assert L.kv4_attn_workspace(1, 1, 4, 2, 64, 16, 2, 1) == 0         # no sequence that long is cut
+    assert L.kv4_attn_workspace(1, 1, 4, 2, 64, 16, 500, 1) > 0
 
 
 def test_rope_refuses_bad_arguments():
