@@ -44,9 +44,6 @@ struct AttnArgs {
 };
 
 constexpr int kTile = 32;      // keys of a step of one wave
-constexpr int kMinRange = 16;  // tiles of a range at least: four for each wave
-constexpr int kBegin = 8;      // what it costs a workgroup to begin and end a segment, in tiles (about 5 us)
-constexpr int kWhole = 48;         // tiles up to which a segment is left whole if no other is longer
 constexpr float kRaise = 8;    // scores (in powers of two) by which a row may pass its reference before that is raised: P < 2^8 in binary16
 
 struct Sequence {
@@ -88,9 +85,9 @@ template <int RB>
 __device__ __forceinline__ int blocks_of(const AttnArgs& a, const Sequence& s) {
     return (s.nq * a.group + RB - 1) / RB;
 }
-// Positions of a segment: kBegin and then its tiles; one without keys has its rows to write and counts as one tile.
+// Positions of a segment: F::begin and then its tiles; one without keys has its rows to write and counts as one tile.
 template <class F>
-__device__ __forceinline__ int positions_of(const Sequence& s) { return kBegin + max(1, (s.len + F::tile - 1) / F::tile); }
+__device__ __forceinline__ int positions_of(const Sequence& s) { return F::begin + max(1, (s.len + F::tile - 1) / F::tile); }
 
 // Where a workgroup begins.
 struct Start {
@@ -117,9 +114,9 @@ __device__ __forceinline__ bool start_of(const AttnArgs& a, int id, Start& at) {
         all += segments * tiles;
         longest = max(longest, tiles);
     }
-    const bool whole = !a.ws || !__any(longest > kBegin + kWhole);
+    const bool whole = !a.ws || !__any(longest > F::begin + F::whole);
     const int W = __builtin_amdgcn_readlane(prefix_sum(all), 63);
-    at.range = whole ? 0 : max(kMinRange, (W + a.target - 1) / a.target);
+    at.range = whole ? 0 : max(F::least, (W + a.target - 1) / a.target);
     if (!whole && id >= a.target) return false;
     const int pos = whole ? id : id * at.range;
     at.first = at.before = 0;
@@ -712,10 +709,13 @@ __device__ __forceinline__ void wide_segment(const AttnArgs& a, const Sequence& 
         }
 }
 
-// The two forms of a segment: NT tiles of 16 rows with the keys shared out to NW waves, or 32 rows to each of NW waves.
+// The two forms of a segment: NT tiles of 16 rows with the keys shared out to NW waves, or 32 rows to each of NW waves.  In tiles: `begin`, what
+// it costs a workgroup to begin and end a segment (about 5 us); `least`, the shortest range; `whole`, up to which a segment is
+// left whole if no other is longer.
 template <int D, int NT, int NW, bool BF>
 struct Narrow {
-    static constexpr int rows = 16 * NT, tile = kTile, waves_simd = NT == 1 ? 4 : NT == 2 ? 2 : 1, threads = 64 * NW;
+    static constexpr int rows = 16 * NT, tile = kTile, waves_simd = NT == 1 ? 4 : 2, threads = 64 * NW;
+    static constexpr int begin = 8, least = 16, whole = 48;
     typedef Shared<D, NT, NW> Lds;
     template <class... A>
     static __device__ __forceinline__ void run(A&&... x) { segment<D, NT, NW, BF>(x...); }
@@ -723,6 +723,7 @@ struct Narrow {
 template <int D, int NW, bool BF>
 struct Wide {
     static constexpr int rows = 32 * NW, tile = kWideTile, waves_simd = 2, threads = 64 * NW;
+    static constexpr int begin = 2, least = 4, whole = 32;
     typedef WideShared<D> Lds;
     template <class... A>
     static __device__ __forceinline__ void run(A&&... x) { wide_segment<D, NW, BF>(x...); }
@@ -745,15 +746,15 @@ __global__ __launch_bounds__(F::threads, F::waves_simd) void attn_kernel(AttnArg
         left = min(at.range, at.total - pos);
     }
     for (;;) {
-        const int w1 = min(of, w0 + left), rb = seg / a.heads;
+        const int w1 = min(of, w0 + left), rb = segments / a.heads - 1 - seg / a.heads;  // the last rows, which see the most, first
         // The keys that the row block's last row sees may be fewer than the sequence has.
         const int most = keys_of(a, s, min((rb + 1) * RB, s.nq * a.group) - 1), tiles = max(1, (most + F::tile - 1) / F::tile);
         int pieces = 1;
         if (at.range) {
-            const int from = at.first + seg * of + kBegin;
+            const int from = at.first + seg * of + F::begin;
             pieces = (from + tiles - 1) / at.range - from / at.range + 1;
         }
-        const int t0 = max(0, w0 - kBegin), t1 = min(tiles, w1 - kBegin);
+        const int t0 = max(0, w0 - F::begin), t1 = min(tiles, w1 - F::begin);
         if (t0 < t1) F::run(a, s, b, seg % a.heads, rb, t0, t1, most, pieces, id + at.before + seg, lds);
         left -= w1 - w0;
         if (left <= 0) return;
@@ -857,9 +858,6 @@ __global__ __launch_bounds__(WAVES > 4 ? 64 * WAVES : 256) void join_kernel(Attn
     }
 }
 
-#ifndef KWW
-#define KWW 8
-#endif
 struct Choice {
     int wide, nt, nw, rows, target;  // wide: 32 rows a wave; otherwise nt tiles of 16 rows
     long long blocks, slots, bytes;
@@ -871,9 +869,9 @@ constexpr int kRanges = 1024;  // four workgroups of 128 registers on each of 25
 Choice choose(long long T, int B, int H, int heads, int d, long long cap, int max_q) {
     const long long rows = (long long)(H / heads) * max_q;
     Choice c;
-    c.wide = rows > 64;
-    c.nt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-    c.nw = c.wide ? (rows <= 128 ? 4 : KWW) : 4;
+    c.wide = rows > 32;
+    c.nt = rows <= 16 ? 1 : 2;
+    c.nw = 4;
     c.rows = c.wide ? 32 * c.nw : 16 * c.nt;
     c.target = c.wide ? 2048 / c.nw : kRanges;
     const long long alone = B * ((rows + c.rows - 1) / c.rows) * heads;
@@ -895,16 +893,15 @@ int check_sizes(long long T, int B, int H, int heads, int d, int page_size, int 
     if (cap > INT_MAX || rows > 1 << 30 || B > 65535 || T * H > INT_MAX) return KV4_EUNSUPPORTED;
     const Choice c = choose(T, B, H, heads, d, cap, max_q);
     // Positions and rows of pieces are counted in 32 bits.
-    return c.blocks >= 1 << 23 || (c.bytes && (double)(c.blocks + c.target) * (double)(cap / kTile + kBegin + kMinRange) > INT_MAX) ? KV4_EUNSUPPORTED : KV4_OK;
+    return c.blocks >= 1 << 23 || (c.bytes && (double)(c.blocks + c.target) * (double)(cap / kTile + 32) > INT_MAX) ? KV4_EUNSUPPORTED : KV4_OK;
 }
 
 template <int D, bool BF>
 int launch_attn(const Choice& c, AttnArgs& a, void* stream) {
-    const void* fn = c.wide      ? (c.nw == 8 ? (const void*)attn_kernel<Wide<D, 8, BF>> : (const void*)attn_kernel<Wide<D, 4, BF>>)
+    const void* fn = c.wide      ? (const void*)attn_kernel<Wide<D, 4, BF>>
                      : c.nw == 16 ? (const void*)attn_kernel<Narrow<D, 1, 16, BF>>
                      : c.nt == 1  ? (const void*)attn_kernel<Narrow<D, 1, 4, BF>>
-                     : c.nt == 2  ? (const void*)attn_kernel<Narrow<D, 2, 4, BF>>
-                                  : (const void*)attn_kernel<Narrow<D, 4, 4, BF>>;
+                                  : (const void*)attn_kernel<Narrow<D, 2, 4, BF>>;
     // Rows enough to fill the units get a wave each, fewer ones four, and the fewest, which have the most pieces, sixteen.
     const long long rows = (long long)a.T * a.H;
     const int waves = rows >= 4096 ? 1 : rows >= 512 ? 4 : 16;
@@ -912,11 +909,9 @@ int launch_attn(const Choice& c, AttnArgs& a, void* stream) {
         constexpr int rb = decltype(RB)::value;
         return waves == 1 ? (const void*)join_kernel<D, rb, BF, 1> : waves == 4 ? (const void*)join_kernel<D, rb, BF, 4> : (const void*)join_kernel<D, rb, BF, 16>;
     };
-    const void* join = c.rows == 16    ? join_of(std::integral_constant<int, 16>())
-                       : c.rows == 32  ? join_of(std::integral_constant<int, 32>())
-                       : c.rows == 64  ? join_of(std::integral_constant<int, 64>())
-                       : c.rows == 128 ? join_of(std::integral_constant<int, 128>())
-                                       : join_of(std::integral_constant<int, 256>());
+    const void* join = c.rows == 16   ? join_of(std::integral_constant<int, 16>())
+                       : c.rows == 32 ? join_of(std::integral_constant<int, 32>())
+                                      : join_of(std::integral_constant<int, 128>());
     void* list[] = {&a};
     if (hipLaunchKernel(fn, dim3((unsigned)c.blocks), dim3(64 * c.nw), list, 0, (hipStream_t)stream) != hipSuccess ||
         (a.ws && hipLaunchKernel(join, dim3((unsigned)(waves == 1 ? (rows + 3) / 4 : rows)), dim3(waves == 16 ? 1024 : 256), list, 0, (hipStream_t)stream) != hipSuccess)) {
