@@ -62,36 +62,40 @@ __device__ __forceinline__ float vector_sum(float x) {
 }
 
 template <int D, bool BF, bool BACK, bool PAIRS>
-__global__ __launch_bounds__(256) void rope_kernel(Args a) {
-    constexpr int L = D / 16, SLOTS = 256 / L, PHASES = SLOTS / kTokens;
-    __shared__ float sums[BACK ? SLOTS * D : 1];
+__global__ __launch_bounds__(256, 4) void rope_kernel(Args a) {
+    constexpr int L = D / 16, SLOTS = 256 / L, PHASES = SLOTS / kTokens, PARTS = 256 / D;
+    __shared__ float sums[BACK ? SLOTS * (D + 4) : 1], parts[BACK ? 256 : 1];
     const int l = threadIdx.x % L, slot = threadIdx.x / L, phase = slot / kTokens;
     const int lo = PAIRS ? 16 * l : 8 * l, hi = PAIRS ? lo + 8 : lo + D / 2;
     const int by = blockIdx.x % a.blocks_y, bx = blockIdx.x / a.blocks_y, step = gridDim.x / a.blocks_y;
     const int h0 = by * a.head_step, h1 = min(h0 + a.head_step, a.t[0].heads + a.t[1].heads);
-    float dw[2][16];
-    if (BACK)
-        for (int i = 0; i < 16; ++i) dw[0][i] = dw[1][i] = 0;
 
-    for (long long first = (long long)bx * kTokens; first < a.tokens; first += (long long)step * kTokens) {
-        const long long token = first + slot % kTokens;
-        if (token >= a.tokens) break;  // no later tile has one for this lane; the lanes of a vector leave together
-        const long long b = token / a.N, n = token % a.N;
-        float c[8], s[8];
-        const int at = a.positions[token];
-        if ((unsigned)at < (unsigned)a.rows) {
-            load8f(a.cos + (long long)at * (D / 2) + 8 * l, c);
-            load8f(a.sin + (long long)at * (D / 2) + 8 * l, s);
-        } else {
-            for (int i = 0; i < 8; ++i) c[i] = s[i] = __uint_as_float(0x7fc00000u);
-        }
+    // One tensor after the other: the weight and its gradient's sums take 32 registers, not 64.
 #pragma unroll
-        for (int z = 0; z < 2; ++z) {
-            const Tensor& T = a.t[z];
-            const int from = z ? max(0, h0 - a.t[0].heads) : h0, to = z ? h1 - a.t[0].heads : min(h1, T.heads);
-            if (from + phase >= to) continue;
-            float w[16];
-            if (T.w) weights<D, BF>(a, T.w, lo, hi, w);
+    for (int z = 0; z < 2; ++z) {
+        const Tensor& T = a.t[z];
+        const int from = z ? max(0, h0 - a.t[0].heads) : h0, to = z ? h1 - a.t[0].heads : min(h1, T.heads);
+        float* const out = BACK && a.ws ? a.ws + ((long long)blockIdx.x * 2 + z) * D : nullptr;
+        if (from >= to) {  // none of this tensor's heads here
+            if (BACK && out && threadIdx.x < D) out[threadIdx.x] = 0;
+            continue;
+        }
+        float w[16], dw[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) w[i] = 1, dw[i] = 0;
+        if (T.w) weights<D, BF>(a, T.w, lo, hi, w);
+        for (long long first = (long long)bx * kTokens; first < a.tokens; first += (long long)step * kTokens) {
+            const long long token = first + slot % kTokens;
+            if (token >= a.tokens) break;  // no later tile has one for this lane; the lanes of a vector leave together
+            const long long b = token / a.N, n = token % a.N;
+            float c[8], s[8];
+            const int at = a.positions[token];
+            if ((unsigned)at < (unsigned)a.rows) {
+                load8f(a.cos + (long long)at * (D / 2) + 8 * l, c);
+                load8f(a.sin + (long long)at * (D / 2) + 8 * l, s);
+            } else {
+                for (int i = 0; i < 8; ++i) c[i] = s[i] = __uint_as_float(0x7fc00000u);
+            }
             const uint16_t* x = T.x + b * T.xs[0] + n * T.xs[1];
             const uint16_t* dy = T.dy + b * T.dys[0] + n * T.dys[1];
             uint16_t* y = T.y + b * T.ys[0] + n * T.ys[1];
@@ -117,7 +121,7 @@ __global__ __launch_bounds__(256) void rope_kernel(Args a) {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const int p = PAIRS ? 2 * i : i, q = PAIRS ? 2 * i + 1 : i + 8;
-                        const float m = T.w ? v[p] * w[p] : v[p], k = T.w ? v[q] * w[q] : v[q];
+                        const float m = v[p] * w[p], k = v[q] * w[q];
                         v[p] = m * c[i] - k * s[i];
                         v[q] = k * c[i] + m * s[i];
                     }
@@ -135,7 +139,7 @@ __global__ __launch_bounds__(256) void rope_kernel(Args a) {
                         float dot = 0;
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
-                            dw[z][i] = fmaf(g[i], v[i], dw[z][i]);
+                            dw[i] = fmaf(g[i], v[i], dw[i]);
                             g[i] *= w[i];
                             dot = fmaf(g[i], v[i], dot);
                         }
@@ -148,18 +152,26 @@ __global__ __launch_bounds__(256) void rope_kernel(Args a) {
                 }
             }
         }
-    }
-    if (!BACK || !a.ws) return;
+        if (!BACK || !out) continue;
+        // The lanes' sums meet in LDS, and 256 / D threads add a column's.
+        float* mine = sums + slot * (D + 4);
 #pragma unroll
-    for (int z = 0; z < 2; ++z) {
-        for (int i = 0; i < 8; ++i) sums[slot * D + lo + i] = dw[z][i], sums[slot * D + hi + i] = dw[z][i + 8];
-        __syncthreads();
-        if (threadIdx.x < D) {
-            float t = 0;
-            for (int i = 0; i < SLOTS; ++i) t += sums[i * D + threadIdx.x];
-            a.ws[((long long)blockIdx.x * 2 + z) * D + threadIdx.x] = t;
+        for (int i = 0; i < 8; i += 4) {
+            *(float4*)(mine + lo + i) = {dw[i], dw[i + 1], dw[i + 2], dw[i + 3]};
+            *(float4*)(mine + hi + i) = {dw[i + 8], dw[i + 9], dw[i + 10], dw[i + 11]};
         }
         __syncthreads();
+        const int c = threadIdx.x % D, part = threadIdx.x / D;
+        float sum = 0;
+#pragma unroll 8
+        for (int i = 0; i < SLOTS / PARTS; ++i) sum += sums[(part * (SLOTS / PARTS) + i) * (D + 4) + c];
+        parts[threadIdx.x] = sum;
+        __syncthreads();
+        if (threadIdx.x < D) {
+            for (int i = 1; i < PARTS; ++i) sum += parts[i * D + threadIdx.x];
+            out[threadIdx.x] = sum;
+        }
+        __syncthreads();  // the next tensor's sums take the place of these
     }
 }
 
@@ -186,13 +198,14 @@ struct Grid {
     int x, y, head_step;
 };
 
-// Token tiles, and the heads cut into as many pieces as it takes to have 1024 workgroups (four on each of 256 units), none smaller than one
-// round of the workgroup's phases; at most 2048 workgroups where their sums have to be added up.
+// Token tiles, and the heads cut into as many pieces as it takes to have 1024 workgroups (four on each of 256 units; backward 512, whose sums are fewer to
+// add: 3 x 1001 tokens of 24 heads, d = 64, 14.6 us against 15.6), none smaller than one round of the workgroup's phases; at most 2048 workgroups where their sums have to be added up.
 Grid grid_of(long long tokens, int heads, int d, bool back) {
     const long long tiles = (tokens + kTokens - 1) / kTokens;
     const int phases = 256 / (d / 16) / kTokens, most = (heads + phases - 1) / phases;
     Grid g;
-    const int want = tiles >= 1024 ? 1 : (int)((1024 + tiles - 1) / tiles);
+    const int enough = back ? 512 : 1024;
+    const int want = tiles >= enough ? 1 : (int)((enough + tiles - 1) / tiles);
     const int pieces = want < most ? want : most;
     g.head_step = ((heads + pieces - 1) / pieces + phases - 1) / phases * phases;
     g.y = (heads + g.head_step - 1) / g.head_step;
