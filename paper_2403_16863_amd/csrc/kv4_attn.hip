@@ -781,15 +781,22 @@ __global__ __launch_bounds__(WAVES > 4 ? 64 * WAVES : 256) void join_kernel(Attn
     if (vec >= (long long)a.T * a.H) return;
     const int t = (int)(vec / a.H);
     const int2 mine_at = a.heads_ws[vec];  // for a row of nobody: anything
-    if (a.cu_q) {
-        int upto = 0;
-        for (int i = lane; i < a.B; i += 64) upto += a.cu_q[i + 1] <= t;
-#pragma unroll
-        for (int d = 32; d; d /= 2) upto += __shfl_xor(upto, d);
-        const int b = __builtin_amdgcn_readfirstlane(upto);
-        if (b >= a.B) return;
-        const Sequence s = shared_sequence(a, b);
-        if (t < s.q0 || t - s.q0 >= s.nq) return;
+    if (a.cu_q) {  // whether the row is somebody's: the sequence is the one with cu_q[b] <= t < cu_q[b + 1]
+        int q0, end;
+        if (a.B < 64) {
+            const int from = a.cu_q[min(lane, a.B)];
+            const int b = __popcll(__ballot(lane > 0 && lane <= a.B && from <= t));
+            if (b >= a.B) return;
+            q0 = __builtin_amdgcn_readlane(from, b), end = __builtin_amdgcn_readlane(from, b + 1);
+        } else {
+            int upto = 0;
+            for (int i = lane; i < a.B; i += 64) upto += a.cu_q[i + 1] <= t;
+            const int b = __builtin_amdgcn_readlane(prefix_sum(upto), 63);
+            if (b >= a.B) return;
+            q0 = a.cu_q[b], end = a.cu_q[b + 1];
+        }
+        q0 = min(max(q0, 0), a.T);  // as in `sequence`
+        if (t < q0 || t - q0 >= min(min(max(end, q0), a.T) - q0, a.max_q)) return;
     }
     const int runs = __builtin_amdgcn_readfirstlane(mine_at.y);
     if (runs == 1) return;
@@ -860,7 +867,7 @@ __global__ __launch_bounds__(WAVES > 4 ? 64 * WAVES : 256) void join_kernel(Attn
 
 struct Choice {
     int wide, nt, nw, rows, target;  // wide: 32 rows a wave; otherwise nt tiles of 16 rows
-    long long blocks, slots, bytes;
+    long long segments, blocks, slots, bytes;
 };
 
 constexpr int kShort = 2048;   // keys
@@ -874,7 +881,7 @@ Choice choose(long long T, int B, int H, int heads, int d, long long cap, int ma
     c.nw = 4;
     c.rows = c.wide ? 32 * c.nw : 16 * c.nt;
     c.target = c.wide ? 2048 / c.nw : kRanges;
-    const long long alone = B * ((rows + c.rows - 1) / c.rows) * heads;
+    const long long alone = c.segments = B * ((rows + c.rows - 1) / c.rows) * heads;
     // Segments that fill the launch by themselves stay whole, and so do those that cannot be long: if they are few, 16 waves take one,
     // up to four tiles each.
     const bool whole = cap <= kShort || alone >= 4 * c.target;
@@ -902,9 +909,9 @@ int launch_attn(const Choice& c, AttnArgs& a, void* stream) {
                      : c.nw == 16 ? (const void*)attn_kernel<Narrow<D, 1, 16, BF>>
                      : c.nt == 1  ? (const void*)attn_kernel<Narrow<D, 1, 4, BF>>
                                   : (const void*)attn_kernel<Narrow<D, 2, 4, BF>>;
-    // Rows enough to fill the units get a wave each, fewer ones four, and the fewest, which have the most pieces, sixteen.
-    const long long rows = (long long)a.T * a.H;
-    const int waves = rows >= 4096 ? 1 : rows >= 512 ? 4 : 16;
+    // A wave takes eight pieces at a time.  A launch's ranges, shared out to its segments, say how many a row has on the average.
+    const long long rows = (long long)a.T * a.H, pieces = c.target / c.segments;
+    const int waves = pieces <= 4 ? 1 : pieces <= 32 ? 4 : 16;
     auto join_of = [&](auto RB) {
         constexpr int rb = decltype(RB)::value;
         return waves == 1 ? (const void*)join_kernel<D, rb, BF, 1> : waves == 4 ? (const void*)join_kernel<D, rb, BF, 4> : (const void*)join_kernel<D, rb, BF, 16>;
