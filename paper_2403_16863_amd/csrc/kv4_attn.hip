@@ -629,20 +629,22 @@ __device__ __forceinline__ void wide_segment(const AttnArgs& a, const Sequence& 
         if (!work) continue;
         const uint4 flags = *(const uint4*)lds.flags[buf];
         const unsigned any = __builtin_amdgcn_readfirstlane(flags.x | flags.y | flags.z | flags.w);
-        if ((t + 1) * kWideTile > least || any) {
-            const unsigned f[4] = {flags.x, flags.y, flags.z, flags.w};
+        if ((t + 1) * kWideTile > least) {
+            const int seen = limit - t * kWideTile - 4 * (int)half;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) x[i][v] = 32 * i + 8 * (v / 4) + v % 4 < seen ? x[i][v] : -INFINITY;
+        }
+        if (__builtin_expect(any != 0, 0)) {
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
                 for (int v = 0; v < 16; ++v) {
                     const int in = 8 * (v / 4) + v % 4;  // token of the 32, less 4 half
-                    const int key = t * kWideTile + 32 * i + in + 4 * (int)half;
-                    x[i][v] = key < limit ? x[i][v] : -INFINITY;
-                    if (any) {
-                        const unsigned g = f[2 * i + in / 16];
-                        if (g >> 16) x[i][v] = -INFINITY;
-                        else if (g >> (in % 16 + 4 * half) & 1 && key < limit) x[i][v] = __uint_as_float(0x7fc00000u);
-                    }
+                    const unsigned f = lds.flags[buf][2 * i + in / 16];
+                    const bool seen = t * kWideTile + 32 * i + in + 4 * (int)half < limit;
+                    x[i][v] = f >> 16 ? -INFINITY : f >> (in % 16 + 4 * half) & 1 && seen ? __uint_as_float(0x7fc00000u) : x[i][v];
                 }
         }
         float top = x[0][0];
