@@ -120,6 +120,25 @@ __device__ __forceinline__ bool start_of(const AttnArgs& a, int id, Start& at) {
     if (!whole && id >= a.target) return false;
     const int pos = whole ? id : id * at.range;
     at.first = at.before = 0;
+    if (whole && a.B > 1 && a.B <= 64) {
+        // Layer by layer: the last row blocks of all sequences, which see the most keys, then those before them.
+        const int blocks = segments / a.heads;
+        auto before = [&](int layer) { return __builtin_amdgcn_readlane(prefix_sum(min(blocks, layer)), 63) * a.heads; };
+        int layer = 0, most = (a.max_q * a.group + F::rows - 1) / F::rows;
+        if (id >= before(most)) return false;
+        while (most - layer > 1) {  // before(layer) <= id < before(most)
+            const int mid = (layer + most) / 2;
+            (before(mid) <= id ? layer : most) = mid;
+        }
+        const int k = (id - before(layer)) / a.heads;
+        const unsigned long long in = __ballot(blocks > layer);
+        const int mine = __builtin_amdgcn_mbcnt_hi((unsigned)(in >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)in, 0));
+        const int l = __builtin_ctzll(__ballot(blocks > layer && mine == k));
+        at.b = l;
+        at.first = id - (layer * a.heads + (id - before(layer)) % a.heads);
+        at.s = {__builtin_amdgcn_readlane(s.len, l), __builtin_amdgcn_readlane(s.q0, l), __builtin_amdgcn_readlane(s.nq, l)};
+        return true;
+    }
     for (int b0 = 0;; b0 += 64) {
         if (a.B > 64) {
             if (b0 >= a.B) return false;
@@ -724,7 +743,7 @@ struct Narrow {
 };
 template <int D, int NW, bool BF>
 struct Wide {
-    static constexpr int rows = 32 * NW, tile = kWideTile, waves_simd = 2, threads = 64 * NW;
+    static constexpr int rows = 32 * NW, tile = kWideTile, waves_simd = D == 64 ? 3 : 2, threads = 64 * NW;
     static constexpr int begin = 2, least = 4, whole = 32;
     typedef WideShared<D> Lds;
     template <class... A>
