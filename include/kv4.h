@@ -49,7 +49,7 @@ enum {
  *                  (a, b) -> (a c - b s, b c + a s)
  *              in fp32, each product and each sum rounded, and from there to 4 bits: the codes are the same as
  *              from these elementary operations.
- *  Limits (KV4_EUNSUPPORTED): T * heads <= 2^31 - 1, pages * page_size <= 2^31 - 1. */
+ *  Limits (KV4_EUNSUPPORTED): T * heads * d < 2^36 (T rounded up to a multiple of 16), pages * page_size <= 2^31 - 1. */
 int kv4_append(const void* k, long long k_token_stride, long long k_head_stride, const void* v, long long v_token_stride,
                long long v_head_stride, void* cache, const int* slots, const float* cos, const float* sin, const int* positions,
                int rows, int interleaved, int T, int heads, int d, int pages, int page_size, int dtype, void* stream);
@@ -65,14 +65,14 @@ int kv4_read(const void* cache, const int* slots, void* k, void* v, int T, int h
  *     x_j = scale * q . k_j,   lse = ln sum_j exp(x_j),   out = sum_j exp(x_j - lse) v_j
  * A row that sees no key gets out = 0 and lse = -infinity.
  *
- *  q, out : device, [T, H, d] contiguous, 16-byte aligned; lse: device, fp32 [T, H].  out must not overlap q.  Rows of q before cu_q[0]
+ *  q, out : device, [T, H, d] contiguous, 16-byte aligned; lse: device, fp32 [T, H].  out must not overlap q, lse or the cache.  Rows of q before cu_q[0]
  *           and from cu_q[B] on belong to nobody: their out and lse stay as they are.
  *  tables : device, int32 [B, width].  Only the entries of pages that hold keys below lens[b] are read; keys of an entry outside
  *           0 .. pages-1 are not seen.  lens: device, int32 [B]; counts above width * page_size are taken as that, negative ones as 0.
  *  cu_q   : device, int32 [B + 1], not decreasing, within 0 .. T, no sequence with more than max_q queries (what exceeds
  *           that is not computed); or null: T / B queries for every sequence, T a multiple of B.
  *  max_q  : the largest number of queries of a sequence (cu_q null: T / B); an upper bound will do, but costs workgroups.
- *  workspace : device, 16-byte aligned, kv4_attn_workspace bytes, any contents, not used by anybody else until the call's
+ *  workspace : device, 16-byte aligned, kv4_attn_workspace bytes (8 T H, and 9 to 68 MB whatever the sequences), any contents, not used by anybody else until the call's
  *           kernels have run; null or fewer bytes: each workgroup goes over all keys of its rows, which is slower for few
  *           long sequences or unequal ones.
  *  Limits (KV4_EUNSUPPORTED): pages * page_size and width * page_size <= 2^31 - 1, T * H <= 2^31 - 1, H / heads * max_q <= 2^30,

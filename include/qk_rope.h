@@ -5,7 +5,7 @@
  * token's position:
  *     r = (mean_i x_i^2 + eps)^(-1/2),   n = r x w,
  *     pair p, channels (i, j) = (p, p + d/2), interleaved != 0: (2p, 2p + 1):   y_i = n_i c_p - n_j s_p,   y_j = n_j c_p + n_i s_p
- * in fp32, rounded once.  Backward, from dy: with g the gradient turned back, h = g w:
+ * in fp32, rounded once (squares too: a head with values beyond 1e18 has r = 0).  Backward, from dy: with g the gradient turned back, h = g w:
  *     dw = sum over tokens and heads of g r x,      dx = r (h - r x mean_i(h_i r x_i)),      without a weight dx = g.
  *
  * General rules (those of attn.h): device pointers are the caller's, nothing is allocated, cleared or waited for, calls are asynchronous
@@ -30,7 +30,8 @@ enum {
 
 /* A tensor of heads: token n of sequence b, head h at data + b * batch_stride + n * token_stride + h * head_stride (in elements), its d
  * channels on end.  data is aligned to 16 bytes and the strides divide by 8 (a stride of a size of 1 is not looked at), so
- * slices of a joint projection and both [B,N,H,d] and [B,H,N,d] will do.  data null: the tensor is left out. */
+ * slices of a joint projection and both [B,N,H,d] and [B,H,N,d] will do; what is
+ * written has no stride of 0.  data null: the tensor is left out. */
 typedef struct {
     void* data;
     long long batch_stride, token_stride, head_stride;

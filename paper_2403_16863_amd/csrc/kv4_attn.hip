@@ -94,7 +94,6 @@ struct Start {
     int range;   // tiles of a range; 0: whole segments
     int b;       // the sequence
     int first;   // position of its first segment
-    int before;  // segments of the sequences before it
     int total;   // positions of all
     Sequence s;
 };
@@ -119,7 +118,7 @@ __device__ __forceinline__ bool start_of(const AttnArgs& a, int id, Start& at) {
     at.range = whole ? 0 : max(F::least, (W + a.target - 1) / a.target);
     if (!whole && id >= a.target) return false;
     const int pos = whole ? id : id * at.range;
-    at.first = at.before = 0;
+    at.first = 0;
     if (whole && a.B > 1 && a.B <= 64) {
         // Layer by layer: the last row blocks of all sequences, which see the most keys, then those before them.
         const int blocks = segments / a.heads;
@@ -150,12 +149,11 @@ __device__ __forceinline__ bool start_of(const AttnArgs& a, int id, Start& at) {
             }
         }
         const int mine = whole ? segments : segments * tiles;
-        const int upto = prefix_sum(mine), segments_upto = prefix_sum(segments);
+        const int upto = prefix_sum(mine);
         const unsigned long long past = __ballot(at.first + upto > pos);
         if (past) {
             const int l = __builtin_ctzll(past);
             at.b = b0 + l;
-            at.before += __builtin_amdgcn_readlane(segments_upto, l) - __builtin_amdgcn_readlane(segments, l);
             at.first += __builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(mine, l);
             at.total = whole ? pos + 1 : W;
             at.s = {__builtin_amdgcn_readlane(s.len, l), __builtin_amdgcn_readlane(s.q0, l), __builtin_amdgcn_readlane(s.nq, l)};
@@ -163,7 +161,6 @@ __device__ __forceinline__ bool start_of(const AttnArgs& a, int id, Start& at) {
         }
         if (a.B <= 64) return false;
         at.first += __builtin_amdgcn_readlane(upto, 63);
-        at.before += __builtin_amdgcn_readlane(segments_upto, 63);
     }
 }
 
@@ -188,7 +185,8 @@ struct Shared {
 };
 
 // Tiles t0 .. t1 - 1 of one segment: row block rb and head h of sequence b.  `pieces` workgroups have a part of it, and this one's goes
-// to `slot` if there are several.
+// to `slot` if there are several: a range has one piece at most that its segment begins with (slot 2 id + 1), its last, and one at
+// most that it does not (slot 2 id), its first.
 template <int D, int NT, int NW, bool BF>
 __device__ __forceinline__ void segment(const AttnArgs& a, const Sequence& s, int b, int h, int rb, int t0, int t1, int most, int pieces, int slot,
                                         Shared<D, NT, NW>& lds) {
@@ -776,15 +774,16 @@ __global__ __launch_bounds__(F::threads, F::waves_simd) void attn_kernel(AttnArg
             pieces = (from + tiles - 1) / at.range - from / at.range + 1;
         }
         const int t0 = max(0, w0 - F::begin), t1 = min(tiles, w1 - F::begin);
-        if (t0 < t1) F::run(a, s, b, seg % a.heads, rb, t0, t1, most, pieces, id + at.before + seg, lds);
+        if (t0 < t1) F::run(a, s, b, seg % a.heads, rb, t0, t1, most, pieces, 2 * id + (t0 == 0), lds);
         left -= w1 - w0;
         if (left <= 0) return;
         __syncthreads();  // the next segment takes this one's place in LDS
         w0 = 0;
         if (++seg < segments) continue;
-        at.first += segments * of, at.before += segments, seg = 0;
-        do {  // positions are left, so a sequence with rows is
-            s = shared_sequence(a, ++b);
+        at.first += segments * of, seg = 0;
+        do {  // positions are left, so a sequence with rows is (unless somebody writes the lengths meanwhile)
+            if (++b >= a.B) return;
+            s = shared_sequence(a, b);
             segments = blocks_of<RB>(a, s) * a.heads;
         } while (!segments);
         of = positions_of<F>(s);
@@ -821,21 +820,23 @@ __global__ __launch_bounds__(WAVES > 4 ? 64 * WAVES : 256) void join_kernel(Attn
     }
     const int runs = __builtin_amdgcn_readfirstlane(mine_at.y);
     if (runs == 1) return;
-    const float* from = a.ws + (long long)__builtin_amdgcn_readfirstlane(mine_at.x) * (D + 2);
-    constexpr long long step = RB * (D + 2);
+    // The first piece's row, an odd slot's; the next ranges' pieces are in even slots.
+    const float* head = a.ws + (long long)__builtin_amdgcn_readfirstlane(mine_at.x) * (D + 2);
+    constexpr long long step = 2 * RB * (D + 2);
+    auto piece = [&](int r) { return head + r * step - (r ? RB * (D + 2) : 0); };
     // Lane l has piece r0 + WAVES l: its reference is raised for 64 pieces at a time.
     float top = -INFINITY, sum = 0, o[C] = {};
     for (int r0 = mine; r0 < runs; r0 += 64 * WAVES) {
         const int r = r0 + WAVES * lane;
         float m = -INFINITY, l = 0;
-        if (r < runs) m = from[r * step + D], l = from[r * step + D + 1];
+        if (r < runs) m = piece(r)[D], l = piece(r)[D + 1];
         const int n = min(64, (runs - r0 + WAVES - 1) / WAVES);
         float x[8][C];
         auto fetch = [&](int k) {
 #pragma unroll
             for (int u = 0; u < 8; ++u)
 #pragma unroll
-                for (int i = 0; i < C; ++i) x[u][i] = from[(r0 + WAVES * min(k + u, n - 1)) * step + lane * C + i];
+                for (int i = 0; i < C; ++i) x[u][i] = piece(r0 + WAVES * min(k + u, n - 1))[lane * C + i];
         };
         fetch(0);  // under way together with the maxima
         float to = m;
@@ -905,10 +906,11 @@ Choice choose(long long T, int B, int H, int heads, int d, long long cap, int ma
     const long long alone = c.segments = B * ((rows + c.rows - 1) / c.rows) * heads;
     // Segments that fill the launch by themselves stay whole, and so do those that cannot be long: if they are few, 16 waves take one,
     // up to four tiles each.
-    const bool whole = cap <= kShort || alone >= 4 * c.target;
+    // The joining kernel has up to 16 waves for each row of q, somebody's or not.
+    const bool whole = cap <= kShort || alone >= 4 * c.target || T * H > 1 << 22;
     if (c.nt == 1 && cap <= kShort && alone <= 256) c.nw = 16;
     c.blocks = whole || alone > c.target ? alone : c.target;
-    c.slots = c.target + alone;
+    c.slots = 2 * c.target;
     c.bytes = whole ? 0 : (T * H * 8 + 15) / 16 * 16 + c.slots * c.rows * (d + 2) * 4;
     return c;
 }
@@ -964,13 +966,14 @@ int kv4_attn(const void* q, const void* cache, const int* tables, const int* len
     if (!q || !cache || !tables || !lens || !out || !lse || T < 0 || pages < 1) return KV4_EINVAL;
     if ((uintptr_t)q % 16 || (uintptr_t)cache % 16 || (uintptr_t)out % 16 || (uintptr_t)workspace % 16) return KV4_EINVAL;
     if ((uintptr_t)tables % 4 || (uintptr_t)lens % 4 || (uintptr_t)cu_q % 4 || (uintptr_t)lse % 4) return KV4_EINVAL;
-    if ((dtype != KV4_F16 && dtype != KV4_BF16) || !isfinite(scale)) return KV4_EINVAL;
+    if ((dtype != KV4_F16 && dtype != KV4_BF16) || !isfinite(scale * 1.4426950408889634f)) return KV4_EINVAL;
     if (T == 0 && B >= 1) return KV4_OK;
     if (!cu_q && (B < 1 || T % B || max_q != T / B)) return KV4_EINVAL;
     if (const int rc = check_sizes(T, B, H, heads, d, page_size, width, max_q)) return rc;
     if ((long long)pages * page_size > INT_MAX) return KV4_EUNSUPPORTED;
     const long long bytes = (long long)T * H * d * 2;
-    if (overlap(q, bytes, out, bytes) || overlap(lse, (long long)T * H * 4, out, bytes)) return KV4_EINVAL;
+    const long long held = (long long)pages * heads * page_size * (d + d / 16);
+    if (overlap(q, bytes, out, bytes) || overlap(lse, (long long)T * H * 4, out, bytes) || overlap(cache, held, out, bytes)) return KV4_EINVAL;
     const Choice c = choose(T, B, H, heads, d, (long long)width * page_size, max_q);
     const bool cut = c.bytes && workspace && workspace_bytes >= c.bytes;
     AttnArgs a = {(const uint16_t*)q, (const uint8_t*)cache, tables, lens, cu_q, (uint16_t*)out, lse, cut ? (int2*)workspace : nullptr,

@@ -199,6 +199,9 @@ int check_cache(const void* cache, int heads, int d, int pages, int page_size) {
     return (long long)pages * page_size > INT_MAX ? KV4_EUNSUPPORTED : KV4_OK;
 }
 
+// Threads of a launch are counted in 32 bits.
+bool too_many(long long T, int heads, int d) { return (T + 15) / 16 * 16 * heads * (d / 16) > 0xffffff00LL; }
+
 int launch(const void* fn, unsigned grid, void* args, void* stream) {
     void* list[] = {args};
     if (hipLaunchKernel(fn, dim3(grid), dim3(256), list, 0, (hipStream_t)stream) != hipSuccess) {
@@ -221,7 +224,7 @@ int kv4_append(const void* k, long long k_token_stride, long long k_head_stride,
     if ((k_token_stride | k_head_stride | v_token_stride | v_head_stride) % 8) return KV4_EINVAL;
     if (!cos != !sin || (cos && (!positions || rows < 1 || (uintptr_t)cos % 16 || (uintptr_t)sin % 16))) return KV4_EINVAL;
     if (const int rc = check_cache(cache, heads, d, pages, page_size)) return rc;
-    if ((long long)T * heads > INT_MAX) return KV4_EUNSUPPORTED;
+    if (too_many(T, heads, d)) return KV4_EUNSUPPORTED;
     if (T == 0) return KV4_OK;
     AppendArgs a = {(const uint16_t*)k, (const uint16_t*)v, k_token_stride, k_head_stride, v_token_stride, v_head_stride, (uint8_t*)cache,
                     slots, cos, sin, positions, rows, interleaved, T, heads, pages * page_size, __builtin_ctz(page_size)};
@@ -237,7 +240,7 @@ int kv4_read(const void* cache, const int* slots, void* k, void* v, int T, int h
     if ((!k && !v) || !slots || T < 0 || (dtype != KV4_F16 && dtype != KV4_BF16)) return KV4_EINVAL;
     if ((uintptr_t)k % 16 || (uintptr_t)v % 16 || (uintptr_t)slots % 4) return KV4_EINVAL;
     if (const int rc = check_cache(cache, heads, d, pages, page_size)) return rc;
-    if ((long long)T * heads > INT_MAX) return KV4_EUNSUPPORTED;
+    if (too_many(T, heads, d)) return KV4_EUNSUPPORTED;
     if (T == 0) return KV4_OK;
     ReadArgs a = {(const uint8_t*)cache, slots, (uint16_t*)k, (uint16_t*)v, T, heads, pages * page_size, __builtin_ctz(page_size)};
     const unsigned grid = (unsigned)((((long long)T + 15) / 16 * 16 * heads * (d / 16) + 255) / 256);

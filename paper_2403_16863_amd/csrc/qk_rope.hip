@@ -214,8 +214,9 @@ Grid grid_of(long long tokens, int heads, int d, bool back) {
     return g;
 }
 
-int check_tensor(const qk_heads* t, int B, int N, int heads) {
+int check_tensor(const qk_heads* t, int B, int N, int heads, bool written) {
     if ((uintptr_t)t->data % 16) return QK_EINVAL;
+    if (written && ((B > 1 && !t->batch_stride) || (N > 1 && !t->token_stride) || (heads > 1 && !t->head_stride))) return QK_EINVAL;
     if ((B > 1 && t->batch_stride % 8) || (N > 1 && t->token_stride % 8) || (heads > 1 && t->head_stride % 8)) return QK_EINVAL;
     return QK_OK;
 }
@@ -261,7 +262,7 @@ int qk_norm_rope(const qk_heads* q, const qk_heads* k, const qk_heads* q_out, co
     const int heads[2] = {H, Hkv};
     for (int z = 0; z < 2; ++z) {
         if (!heads[z]) continue;
-        if (check_tensor(in[z], B, N, heads[z]) || check_tensor(out[z], B, N, heads[z])) return QK_EINVAL;
+        if (check_tensor(in[z], B, N, heads[z], false) || check_tensor(out[z], B, N, heads[z], true)) return QK_EINVAL;
         a.t[z].x = (const uint16_t*)in[z]->data, a.t[z].y = (uint16_t*)out[z]->data, a.t[z].w = w[z], a.t[z].heads = heads[z];
         strides(in[z], a.t[z].xs), strides(out[z], a.t[z].ys);
     }
@@ -307,7 +308,8 @@ int qk_norm_rope_bwd(const qk_heads* dq_out, const qk_heads* dk_out, const qk_he
     for (int z = 0; z < 2; ++z) {
         if (!heads[z]) continue;
         if (w[z] && !given(x[z])) return QK_EINVAL;
-        if (check_tensor(dy[z], B, N, heads[z]) || check_tensor(dx[z], B, N, heads[z]) || (w[z] && check_tensor(x[z], B, N, heads[z]))) return QK_EINVAL;
+        if (check_tensor(dy[z], B, N, heads[z], false) || check_tensor(dx[z], B, N, heads[z], true) || (w[z] && check_tensor(x[z], B, N, heads[z], false)))
+            return QK_EINVAL;
         if (w[z]) a.t[z].x = (const uint16_t*)x[z]->data, strides(x[z], a.t[z].xs);
         a.t[z].dy = (const uint16_t*)dy[z]->data, a.t[z].y = (uint16_t*)dx[z]->data, a.t[z].w = w[z], a.t[z].heads = heads[z];
         strides(dy[z], a.t[z].dys), strides(dx[z], a.t[z].ys);

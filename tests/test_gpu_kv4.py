@@ -207,6 +207,38 @@ def test_many_sequences_and_rows_of_nobody():
         assert torch.isnan(x[:5]).all() and torch.isnan(x[155:]).all()
 
 
+def random_case(B, most, most_q, H, heads, d, seed, empty=4):
+    """Lengths of all sizes, some of them and some numbers of queries zero."""
+    r = np.random.default_rng(seed)
+    lens = [0 if r.integers(empty + 6) == 0 else int(most ** r.uniform(0, 1)) for _ in range(B)]
+    nqs = [0 if r.integers(empty) == 0 else int(r.integers(1, most_q + 1)) for _ in range(B)]
+    lens[B // 2], nqs[B // 2] = most, most_q
+    return lens, nqs, H, heads, d, 16, True
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("B,most,most_q,H,heads,d", [
+    (70, 2600, 1, 4, 2, 64), (130, 2600, 2, 4, 1, 128),            # ranges over more sequences than a wave has lanes
+    (9, 4100, 3, 6, 2, 128), (9, 4100, 9, 6, 2, 64),               # ranges that end inside, at and behind sequences, some without rows
+    (5, 3000, 50, 4, 2, 64), (6, 2300, 90, 4, 1, 128),             # the same of many rows
+    (66, 300, 40, 2, 1, 64), (64, 200, 60, 3, 1, 128), (3, 500, 150, 2, 2, 64),     # whole row blocks, in layers and not
+])
+def test_unequal_sequences(B, most, most_q, H, heads, d, dtype):
+    s = setup(random_case(B, most, most_q, H, heads, d, B + d), dtype, seed=B)
+    want = reference(s)
+    check(*run(s), want, dtype, scores=60)
+    s["causal"] = False
+    check(*run(s), reference(s), dtype, scores=60)
+
+
+def test_lengths_at_the_edges_of_a_range():
+    """The shortest ranges, with lengths around their ends: every piece of a row has to be joined, once."""
+    for d, q in ((64, 1), (128, 40)):
+        for n in (2049, 2080, 2081, 2112, 2500, 3000, 3500, 4096):
+            s = setup(([n], [q], 1, 1, d, 64, True), torch.float16, seed=n)
+            check(*run(s), reference(s), torch.float16, scores=60)
+
+
 def test_pages_outside_the_cache_are_not_seen_and_lengths_are_limited():
     s = setup(([100, 100, 100], [3, 3, 3], 4, 2, 64, 16, True), torch.float16)
     s["tables"][0, 1] = -1
