@@ -1,16 +1,23 @@
 // Attention over the paged 4-bit cache (include/kv4.h has the operation and the format).
 //
-// A workgroup takes RB = 16 NT rows (query i and head of the group: row = i * group + head) of one sequence and one head of the
-// cache over a run of keys, and goes once over them with the running maximum and sum of the softmax.  Its four waves take
-// turns at tiles of 32 keys, each with statistics and an output of its own; they meet at the end.  Tiles stay in
-// registers: a lane's 16 bytes of key codes are one token's block of 32 channels under one scale, which is also what the
-// 16 x 16 x 32 MFMA wants as rows of its first operand once the channels are taken in this order on both sides; the conversion
-// instruction takes two codes and their scale to two binary16 values, exactly, at the rate of any other vector instruction.
+// Rows (query i and head of the group: row = i * group + head) of one sequence and one head of the cache share its keys, and a workgroup
+// goes once over a run of them with the running maximum and sum of the softmax.  There are two forms.
+//
+// Up to 32 rows (`segment`): 16 or 32 rows a workgroup, whose waves take turns at tiles of 32 keys, each with statistics and an
+// output of its own; they meet at the end.  Tiles stay in registers: a lane's 16 bytes of key codes are one token's block of 32 channels under one
+// scale, which is also what the 16 x 16 x 32 MFMA wants as rows of its first operand once the channels are taken in this order on both
+// sides; the conversion instruction takes two codes and their scale to two binary16 values, exactly, at the rate of any other vector
+// instruction (2.1 ns a wave on each of four units).
 //     S^T (16 tokens x 16 rows) = K Q^T:  lane l has row l % 16 of Q and tokens 4 (l / 16) .. + 3
 //     O^T (16 channels x 16 rows) += V^T P^T: the second operand is P as S^T leaves it, so lane l's tokens are 4 (l / 16) .. + 3 of
 //     each of two groups of 16, and the cache holds the values in quads of tokens for that reason.
+// Memory binds long calls: the loop reads 6.3 TB/s (64 sequences of up to 8192 keys); a launch's beginnings, ends and second kernel are the rest.
+// More rows (`wide_segment`): 128 a workgroup, tiles of 64 keys converted once into LDS; its products and the softmax's vector
+// instructions bind it (984 TFLOP/s for 2048 queries behind 14336 keys, 32 heads on 8, d = 128).
+//
 // All values of the cache are exact in binary16, so one kernel serves both types: bfloat16 queries become binary16 relative to
-// the power of two of their row's largest element.
+// the power of two of their row's largest element.  (The MFMA that takes the codes and scales themselves, with the queries as
+// sums of e4m3 terms, has sums that are off by 4e-5 of sum |q k|: too far for scores.)
 //
 // The keys of all sequences are dealt on the device, from the lengths that the launch finds in memory (a captured launch meets new ones
 // at every replay).  A segment is a sequence, a block of rows and a head; all segments' tiles on end are cut into ranges of one length, one for
@@ -43,8 +50,8 @@ struct AttnArgs {
     int target;      // ranges that a launch is cut into at most
 };
 
-constexpr int kTile = 32;      // keys of a step of one wave
-constexpr float kRaise = 8;    // scores (in powers of two) by which a row may pass its reference before that is raised: P < 2^8 in binary16
+constexpr int kTile = 32;    // keys of a step of one wave
+constexpr float kRaise = 8;  // scores (in powers of two) by which a row may pass its reference before that is raised: P < 2^8 in binary16
 
 struct Sequence {
     int len, q0, nq;
@@ -729,8 +736,8 @@ __device__ __forceinline__ void wide_segment(const AttnArgs& a, const Sequence& 
 }
 
 // The two forms of a segment: NT tiles of 16 rows with the keys shared out to NW waves, or 32 rows to each of NW waves.  In tiles: `begin`, what
-// it costs a workgroup to begin and end a segment (about 5 us); `least`, the shortest range; `whole`, up to which a segment is
-// left whole if no other is longer.
+// it costs a workgroup to begin and end a segment (about 5 us; 0, 4, 8, 16 tiles: 64 sequences of up to 8192 keys 80, 76, 74.5, 74.3 us, 8 of up to
+// 4000 19.2, 16.6, 15.5, 15.4); `least`, the shortest range; `whole`, up to which a segment is left whole if no other is longer.
 template <int D, int NT, int NW, bool BF>
 struct Narrow {
     static constexpr int rows = 16 * NT, tile = kTile, waves_simd = NT == 1 ? 4 : 2, threads = 64 * NW;
@@ -892,8 +899,14 @@ struct Choice {
     long long segments, blocks, slots, bytes;
 };
 
-constexpr int kShort = 2048;   // keys
-constexpr int kRanges = 1024;  // four workgroups of 128 registers on each of 256 units
+// Both sides of the choices, in us (bfloat16, d = 128, 32 heads on 8 unless said; forms timed in turn on one card):
+//  * rows from 33 on in the wide form, not four tiles of 16 rows a wave: 40 rows over four caches of up to 20000 keys 39 against 73, 64 over the
+//    same 30 against 52.  24 rows: 33 against 34 in two tiles of 16, with d = 64 29 against 26.
+//  * kRanges: 768, 1024, 1536, 2048 ranges: 64 sequences of up to 8192 keys 83, 80, 83, 82; two of up to 131072 40, 42, 47, 49.  Eight waves a workgroup
+//    and half the ranges: 87 and 40.
+//  * kShort: caches of 1500 keys cut all the same: 64 sequences 23 against 20, one of 1003 keys 11.7 against 10.9 with its 16 waves, prompts 39 against 31.
+constexpr int kShort = 2048;   // keys up to which nothing is cut
+constexpr int kRanges = 1024;  // four workgroups of 128 registers on each of 256 units; two of the wide form
 
 Choice choose(long long T, int B, int H, int heads, int d, long long cap, int max_q) {
     const long long rows = (long long)(H / heads) * max_q;
@@ -901,8 +914,8 @@ Choice choose(long long T, int B, int H, int heads, int d, long long cap, int ma
     c.wide = rows > 32;
     c.nt = rows <= 16 ? 1 : 2;
     c.nw = 4;
-    c.rows = c.wide ? 32 * c.nw : 16 * c.nt;
-    c.target = c.wide ? 2048 / c.nw : kRanges;
+    c.rows = c.wide ? 128 : 16 * c.nt;
+    c.target = c.wide ? kRanges / 2 : kRanges;
     const long long alone = c.segments = B * ((rows + c.rows - 1) / c.rows) * heads;
     // Segments that fill the launch by themselves stay whole, and so do those that cannot be long: if they are few, 16 waves take one,
     // up to four tiles each.
