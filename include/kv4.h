@@ -72,7 +72,7 @@ int kv4_read(const void* cache, const int* slots, void* k, void* v, int T, int h
  *  cu_q   : device, int32 [B + 1], not decreasing, within 0 .. T, no sequence with more than max_q queries (what exceeds
  *           that is not computed); or null: T / B queries for every sequence, T a multiple of B.
  *  max_q  : the largest number of queries of a sequence (cu_q null: T / B); an upper bound will do, but costs workgroups.
- *  workspace : device, 16-byte aligned, kv4_attn_workspace bytes (8 T H, and 9 to 68 MB whatever the sequences), any contents, not used by anybody else until the call's
+ *  workspace : device, 16-byte aligned, kv4_attn_workspace bytes (8 T H, and 9 to 69 MB whatever the sequences), any contents, not used by anybody else until the call's
  *           kernels have run; null or fewer bytes: each workgroup goes over all keys of its rows, which is slower for few
  *           long sequences or unequal ones.
  *  Limits (KV4_EUNSUPPORTED): pages * page_size and width * page_size <= 2^31 - 1, T * H <= 2^31 - 1, H / heads * max_q <= 2^30,

@@ -904,9 +904,10 @@ struct Choice {
 //    same 30 against 52.  24 rows: 33 against 34 in two tiles of 16, with d = 64 29 against 26.
 //  * kRanges: 768, 1024, 1536, 2048 ranges: 64 sequences of up to 8192 keys 83, 80, 83, 82; two of up to 131072 40, 42, 47, 49.  Eight waves a workgroup
 //    and half the ranges: 87 and 40.
+//    Forms of which two workgroups fill a unit, 1024 and 512: 24 rows over 16 caches of up to 6000 keys 34, 26, the same of 32 rows, d = 64, 26, 21.5.
 //  * kShort: caches of 1500 keys cut all the same: 64 sequences 23 against 20, one of 1003 keys 11.7 against 10.9 with its 16 waves, prompts 39 against 31.
 constexpr int kShort = 2048;   // keys up to which nothing is cut
-constexpr int kRanges = 1024;  // four workgroups of 128 registers on each of 256 units; two of the wide form
+constexpr int kRanges = 1024;  // four workgroups of 128 registers on each of 256 units; of the other forms two, and half the ranges
 
 Choice choose(long long T, int B, int H, int heads, int d, long long cap, int max_q) {
     const long long rows = (long long)(H / heads) * max_q;
@@ -915,7 +916,7 @@ Choice choose(long long T, int B, int H, int heads, int d, long long cap, int ma
     c.nt = rows <= 16 ? 1 : 2;
     c.nw = 4;
     c.rows = c.wide ? 128 : 16 * c.nt;
-    c.target = c.wide ? kRanges / 2 : kRanges;
+    c.target = c.wide || c.nt == 2 ? kRanges / 2 : kRanges;
     const long long alone = c.segments = B * ((rows + c.rows - 1) / c.rows) * heads;
     // Segments that fill the launch by themselves stay whole, and so do those that cannot be long: if they are few, 16 waves take one,
     // up to four tiles each.

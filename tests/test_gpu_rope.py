@@ -88,6 +88,9 @@ def test_one_tensor_in_place_and_positions_outside_the_table(d):
     mine = q.clone()
     rope.qk_norm_rope(mine, None, mine, None, c, s, positions, qw)
     assert torch.equal(mine.view(torch.int16), want.view(torch.int16))
+    alone = torch.empty_like(want)
+    rope.qk_norm_rope(None, q, None, alone, c, s, positions, None, qw)     # as keys, without queries
+    assert torch.equal(alone.view(torch.int16), want.view(torch.int16))
     both, ko = torch.empty_like(want), torch.empty(2, 11, 2, d, dtype=torch.bfloat16, device="cuda")
     rope.qk_norm_rope(q, k, both, ko, c, s, positions, qw)          # a norm for the queries alone
     assert torch.equal(both.view(torch.int16), want.view(torch.int16))
