@@ -5,7 +5,7 @@
  * token's position:
  *     r = (mean_i x_i^2 + eps)^(-1/2),   n = r x w,
  *     pair p, channels (i, j) = (p, p + d/2), interleaved != 0: (2p, 2p + 1):   y_i = n_i c_p - n_j s_p,   y_j = n_j c_p + n_i s_p
- * in fp32, rounded once (squares too: a head with values beyond 1e18 has r = 0).  Backward, from dy: with g the gradient turned back, h = g w:
+ * in fp32, rounded once (squares too: a head with values beyond 1e18 has r = 0, and with eps = 0 one of values below 1e-19 has r = infinity).  Backward, from dy: with g the gradient turned back, h = g w:
  *     dw = sum over tokens and heads of g r x,      dx = r (h - r x mean_i(h_i r x_i)),      without a weight dx = g.
  *
  * General rules (those of attn.h): device pointers are the caller's, nothing is allocated, cleared or waited for, calls are asynchronous

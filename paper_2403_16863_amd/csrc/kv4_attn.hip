@@ -920,8 +920,8 @@ Choice choose(long long T, int B, int H, int heads, int d, long long cap, int ma
     const long long alone = c.segments = B * ((rows + c.rows - 1) / c.rows) * heads;
     // Segments that fill the launch by themselves stay whole, and so do those that cannot be long: if they are few, 16 waves take one,
     // up to four tiles each.
-    // The joining kernel has up to 16 waves for each row of q, somebody's or not.
-    const bool whole = cap <= kShort || alone >= 4 * c.target || T * H > 1 << 22;
+    // The joining kernel has up to 16 waves for each row of q, somebody's or not, and threads of a launch are counted in 32 bits.
+    const bool whole = cap <= kShort || alone >= 4 * c.target || T * H >= 1 << 22;
     if (c.nt == 1 && cap <= kShort && alone <= 256) c.nw = 16;
     c.blocks = whole || alone > c.target ? alone : c.target;
     c.slots = 2 * c.target;
@@ -934,9 +934,9 @@ int check_sizes(long long T, int B, int H, int heads, int d, int page_size, int 
     if (page_size < 16 || page_size > 65536 || (page_size & (page_size - 1))) return KV4_EINVAL;
     if (d != 64 && d != 128) return KV4_EUNSUPPORTED;
     const long long cap = (long long)width * page_size, rows = (long long)(H / heads) * max_q;
-    if (cap > INT_MAX || rows > 1 << 30 || B > 65535 || T * H > INT_MAX) return KV4_EUNSUPPORTED;
+    if (cap > INT_MAX - 65535 || rows > 1 << 30 || B > 65535 || T * H > INT_MAX) return KV4_EUNSUPPORTED;
     const Choice c = choose(T, B, H, heads, d, cap, max_q);
-    // Positions and rows of pieces are counted in 32 bits.
+    // Positions and rows of pieces are counted in 32 bits, and so are keys up to the end of the last tile.
     return c.blocks >= 1 << 23 || (c.bytes && (double)(c.blocks + c.target) * (double)(cap / kTile + 32) > INT_MAX) ? KV4_EUNSUPPORTED : KV4_OK;
 }
 

@@ -224,12 +224,12 @@ def kv4_attn(q, cache, tables, lens, out, lse, causal: bool, scale: float, cu_q=
         _ints("cu_q", cu_q, (B + 1,))
         if max_q is None:
             raise ValueError("cu_q needs max_q, the largest number of queries of a sequence")
-    elif B == 0 or T % B or (max_q is not None and max_q != T // B):
+    elif (B == 0 and T) or (B and T % B) or (B and max_q is not None and max_q != T // B):
         raise ValueError("without cu_q every sequence has T / B queries")
-    else:
-        max_q = T // B
     if T == 0:
         return
+    if cu_q is None:
+        max_q = T // B
     st = _stream(stream, cache.device)
     need = kv4_attn_workspace(T, B, H, heads, d, page_size, width, max_q)
     if workspace is not None:

@@ -134,3 +134,21 @@ def test_python_refusals_name_the_argument():
             rope.qk_norm_rope_bwd(x, None, x, None, x, None, cos, cos, pos, w)
         with pytest.raises(ValueError, match="forward's input"):
             rope.qk_norm_rope_bwd(x, None, None, None, x, None, cos, cos, pos, w, None, w.float())
+
+
+def test_sizes_at_the_limits_of_32_bits():
+    """No launch of 2^32 threads (16 waves to each of 2^22 rows of q), no tile whose end passes 2^31 keys, no sequences at all."""
+    L = kv4.lib()
+    assert L.kv4_attn_workspace(1 << 17, 1, 32, 8, 64, 16, 500, 1) == 0
+    assert L.kv4_attn_workspace((1 << 17) - 1, 1, 32, 8, 64, 16, 500, 1) > 0
+    many = 1 << 14                                                       # segments enough to stay whole
+    assert L.kv4_attn_workspace(many, many, 8, 8, 64, 65536, 32767, 1) == 0
+    assert L.kv4_attn_workspace(many, many, 8, 8, 64, 16, (1 << 27) - 4096, 1) == 0
+    assert L.kv4_attn_workspace(many, many, 8, 8, 64, 16, (1 << 27) - 4095, 1) == kv4.KV4_EUNSUPPORTED
+    from torch._subclasses.fake_tensor import FakeTensorMode
+    with FakeTensorMode():
+        z = lambda *s, dtype=torch.float16: torch.empty(*s, dtype=dtype, device="cuda")  # noqa: E731
+        i32, f32 = torch.int32, torch.float32
+        cache, q = z(3, 2, 16, 68, dtype=torch.uint8), z(0, 4, 64)
+        kv4.kv4_attn(q, cache, z(0, 5, dtype=i32), z(0, dtype=i32), q, z(0, 4, dtype=f32), True, 1.0)
+        kv4.kv4_attn(q, cache, z(2, 5, dtype=i32), z(2, dtype=i32), q, z(0, 4, dtype=f32), True, 1.0)
