@@ -12,8 +12,9 @@
 //     O^T (16 channels x 16 rows) += V^T P^T: the second operand is P as S^T leaves it, so lane l's tokens are 4 (l / 16) .. + 3 of
 //     each of two groups of 16, and the cache holds the values in quads of tokens for that reason.
 // Memory binds long calls: the loop reads 6.3 TB/s (64 sequences of up to 8192 keys); a launch's beginnings, ends and second kernel are the rest.
-// More rows (`wide_segment`): 128 a workgroup, tiles of 64 keys converted once into LDS; its products and the softmax's vector
-// instructions bind it (984 TFLOP/s for 2048 queries behind 14336 keys, 32 heads on 8, d = 128).
+// More rows (`wide_segment`): 128 or 256 a workgroup, tiles of 64 keys converted once into LDS, the next tile's scores multiplied during this one's
+// softmax.  The card's power binds it (1085 TFLOP/s for 2048 queries behind 14336 keys, 32 heads on 8, d = 128): its matrix instructions run at 2500
+// TFLOP/s on constant data, on random data at 1700, and at 1390 with a read of LDS, an exponential and four more vector instructions to each.
 //
 // All values of the cache are exact in binary16, so one kernel serves both types: bfloat16 queries become binary16 relative to
 // the power of two of their row's largest element.  (The MFMA that takes the codes and scales themselves, with the queries as
@@ -463,7 +464,8 @@ __device__ __forceinline__ void segment(const AttnArgs& a, const Sequence& s, in
 
 // Many rows: a wave has 32 rows, all waves go over the same tiles of 64 keys, and the converted tile lies in LDS, in the order in which
 // the 32 x 32 x 16 MFMA takes its first operand, so that 16 bytes of a lane are one read.  A tile is converted once for the workgroup's
-// rows, one ahead of its use, from bytes that were asked for another one ahead.
+// rows, from bytes that were asked for a tile ahead, the keys two tiles ahead of their softmax and the values one: while a tile's
+// exponentials run, the next one's scores are multiplied between them (one after the other: 2048 queries behind as many keys 55 us, so 52).
 //     S^T (32 tokens x 32 rows) = K Q^T:  lane l has row l % 32 of Q, register v token 8 (v / 4) + 4 (l / 32) + v % 4
 //     O^T (32 channels x 32 rows) += V^T P^T: P as S^T leaves it, so half l / 32 has tokens 4 (l / 32) .. + 3 and 8 + 4 (l / 32) .. + 3 of 16
 // A row's output stays in one wave: nothing to join within the workgroup.
@@ -501,87 +503,88 @@ __device__ __forceinline__ void wide_segment(const AttnArgs& a, const Sequence& 
     unsigned rk[W], rv[W], rks = 0, rvs = 0;
     const unsigned k_off = c16 * (D / 2) + quad * (D / 8), ks_off = Group<D>::k_scales + c16 * (D / 32) + quad * (D / 4) / 32;
     const unsigned v_off = Group<D>::v_codes + quad * (2 * D) + c16 * (D / 8), vs_off = Group<D>::v_scales + quad * (D / 8) + c16 * (D / 16) / 32 * 4;
-    auto fetch = [&](const uint8_t* at) {
-        if (keys) {
-            const unsigned* k = (const unsigned*)(at + k_off);
+    auto fetch_k = [&](const uint8_t* at) {
+        if (!keys) return;
+        const unsigned* k = (const unsigned*)(at + k_off);
 #pragma unroll
-            for (int w = 0; w < W; ++w) rk[w] = k[w];
-            rks = at[ks_off];
-        }
-        if (vals) {
-            const unsigned* v = (const unsigned*)(at + v_off);
+        for (int w = 0; w < W; ++w) rk[w] = k[w];
+        rks = at[ks_off];
+    };
+    auto fetch_v = [&](const uint8_t* at) {
+        if (!vals) return;
+        const unsigned* v = (const unsigned*)(at + v_off);
 #pragma unroll
-            for (int w = 0; w < W; ++w) rv[w] = v[w];
-            rvs = *(const unsigned*)(at + vs_off);
+        for (int w = 0; w < W; ++w) rv[w] = v[w];
+        rvs = *(const unsigned*)(at + vs_off);
+    };
+    auto put_k = [&](int t) {  // the lane's token and D/4 channels from quad * D/4
+        if (!keys) return;
+        uint4* to = lds.k[t & 1] + ((mine_g >> 1) * KS * 64 + (mine_g & 1) * 16 + c16);
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            const unsigned piece = quad * W + w;  // 8 channels: half piece % 2 of 16
+            to[(piece >> 1) * 64 + (piece & 1) * 32] = values8<false>(rk[w], rks << 23);
         }
     };
-    auto put = [&](int t, int page) {
-        const int buf = t & 1;
-        if (keys) {  // the lane's token and D/4 channels from quad * D/4
-            uint4* to = lds.k[buf] + ((mine_g >> 1) * KS * 64 + (mine_g & 1) * 16 + c16);
+    auto put_v = [&](int t, int page) {
+        if (!vals) return;
+        const int buf = t & 1, key = t * kWideTile + 16 * mine_g + 4 * (int)quad;
+        const bool there = (unsigned)page < (unsigned)a.pages;
+        if (!there || t * kWideTile + 16 * mine_g + 16 > most) {
+            const int live = there ? most - key : 0;
+            const unsigned keep = live >= 4 ? ~0u : live <= 0 ? 0u : (1u << (8 * live)) - 1;
+            rvs = (rvs & keep) | (0x7f7f7f7fu & ~keep);
 #pragma unroll
-            for (int w = 0; w < W; ++w) {
-                const unsigned piece = quad * W + w;  // 8 channels: half piece % 2 of 16
-                to[(piece >> 1) * 64 + (piece & 1) * 32] = values8<false>(rk[w], rks << 23);
+            for (int w = 0; w < W; ++w)
+                rv[w] = D == 128 ? (w < live ? rv[w] : 0) : rv[w] & ((2 * w < live ? 0xffffu : 0u) | (2 * w + 1 < live ? 0xffff0000u : 0u));
+        }
+        // A NaN must reach the rows that see its token and no other: it goes into their scores, and its codes are cleared.
+        unsigned flags = there ? 0 : 1u << 16;
+        if (__builtin_expect(__any((((rvs & 0x7f7f7f7fu) + 0x01010101u) & rvs & 0x80808080u) != 0), 0)) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const bool bad = (rvs >> (8 * j) & 255u) == 255u;
+                const unsigned long long all = __ballot(bad);
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    if (all >> (16 * q) & 0xffffu) flags |= 1u << (4 * q + j);
+                if (bad) rvs &= ~(0x80u << (8 * j));
+                if (D == 128) rv[j % W] = bad ? 0 : rv[j % W];
+                else rv[j / 2] &= bad ? (j % 2 ? 0xffffu : 0xffff0000u) : ~0u;
             }
         }
-        if (vals) {
-            const int key = t * kWideTile + 16 * mine_g + 4 * (int)quad;
-            const bool there = (unsigned)page < (unsigned)a.pages;
-            if (!there || t * kWideTile + 16 * mine_g + 16 > most) {
-                const int live = there ? most - key : 0;
-                const unsigned keep = live >= 4 ? ~0u : live <= 0 ? 0u : (1u << (8 * live)) - 1;
-                rvs = (rvs & keep) | (0x7f7f7f7fu & ~keep);
-#pragma unroll
-                for (int w = 0; w < W; ++w)
-                    rv[w] = D == 128 ? (w < live ? rv[w] : 0) : rv[w] & ((2 * w < live ? 0xffffu : 0u) | (2 * w + 1 < live ? 0xffff0000u : 0u));
-            }
-            // A NaN must reach the rows that see its token and no other: it goes into their scores, and its codes are cleared.
-            unsigned flags = there ? 0 : 1u << 16;
-            if (__builtin_expect(__any((((rvs & 0x7f7f7f7fu) + 0x01010101u) & rvs & 0x80808080u) != 0), 0)) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const bool bad = (rvs >> (8 * j) & 255u) == 255u;
-                    const unsigned long long all = __ballot(bad);
-#pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        if (all >> (16 * q) & 0xffffu) flags |= 1u << (4 * q + j);
-                    if (bad) rvs &= ~(0x80u << (8 * j));
-                    if (D == 128) rv[j % W] = bad ? 0 : rv[j % W];
-                    else rv[j / 2] &= bad ? (j % 2 ? 0xffffu : 0xffff0000u) : ~0u;
-                }
-            }
-            if (lane == 0) lds.flags[buf][mine_g] = flags;
-            const unsigned sc[4] = {rvs << 23, rvs << 15, rvs << 7, rvs >> 1};
-            // Four tokens of a channel are 8 bytes: half quad % 2, the lower or upper 8 bytes of the lane's 16 by quad / 2.
-            uint2* to = (uint2*)lds.v[buf] + (mine_g * CT * 64 + (quad & 1) * 32 + c16) * 2 + (quad >> 1);
-            auto channels = [&](auto SEL) {
-                constexpr int c = decltype(SEL)::value;
-                unsigned two[4];
-                if constexpr (D == 128) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) two[j] = values2<false, c>(rv[j % W], sc[j]);
-                } else {
-                    two[0] = values2<false, c>(rv[0], sc[0]), two[1] = values2<false, 2 + c>(rv[0], sc[1]);
-                    two[2] = values2<false, c>(rv[1], sc[2]), two[3] = values2<false, 2 + c>(rv[1], sc[3]);
-                }
-                to[c * 128] = uint2{__builtin_amdgcn_perm(two[1], two[0], 0x05040100u), __builtin_amdgcn_perm(two[3], two[2], 0x05040100u)};
-                to[c * 128 + 32] = uint2{__builtin_amdgcn_perm(two[1], two[0], 0x07060302u), __builtin_amdgcn_perm(two[3], two[2], 0x07060302u)};
-            };
-            channels(std::integral_constant<int, 0>());
-            channels(std::integral_constant<int, 1>());
+        if (lane == 0) lds.flags[buf][mine_g] = flags;
+        const unsigned sc[4] = {rvs << 23, rvs << 15, rvs << 7, rvs >> 1};
+        // Four tokens of a channel are 8 bytes: half quad % 2, the lower or upper 8 bytes of the lane's 16 by quad / 2.
+        uint2* to = (uint2*)lds.v[buf] + (mine_g * CT * 64 + (quad & 1) * 32 + c16) * 2 + (quad >> 1);
+        auto channels = [&](auto SEL) {
+            constexpr int c = decltype(SEL)::value;
+            unsigned two[4];
             if constexpr (D == 128) {
-                channels(std::integral_constant<int, 2>());
-                channels(std::integral_constant<int, 3>());
+#pragma unroll
+                for (int j = 0; j < 4; ++j) two[j] = values2<false, c>(rv[j % W], sc[j]);
+            } else {
+                two[0] = values2<false, c>(rv[0], sc[0]), two[1] = values2<false, 2 + c>(rv[0], sc[1]);
+                two[2] = values2<false, c>(rv[1], sc[2]), two[3] = values2<false, 2 + c>(rv[1], sc[3]);
             }
+            to[c * 128] = uint2{__builtin_amdgcn_perm(two[1], two[0], 0x05040100u), __builtin_amdgcn_perm(two[3], two[2], 0x05040100u)};
+            to[c * 128 + 32] = uint2{__builtin_amdgcn_perm(two[1], two[0], 0x07060302u), __builtin_amdgcn_perm(two[3], two[2], 0x07060302u)};
+        };
+        channels(std::integral_constant<int, 0>());
+        channels(std::integral_constant<int, 1>());
+        if constexpr (D == 128) {
+            channels(std::integral_constant<int, 2>());
+            channels(std::integral_constant<int, 3>());
         }
     };
 
-    int page = -1, ahead = -1;
+    int pages[3] = {-1, -1, -1};  // of the wave's groups in the tiles t + 1, t + 2 and t + 3
+    int ahead = -1;
     if (t0 < t1) {
-        page = page_of(4 * t0 + mine_g);
-        ahead = page_of(4 * (t0 + 1) + mine_g);
-        fetch(group_at(4 * t0 + mine_g, page));
+        for (int i = 0; i < 3; ++i) pages[i] = page_of(4 * (t0 + i) + mine_g);
+        ahead = page_of(4 * (t0 + 3) + mine_g);
+        fetch_k(group_at(4 * t0 + mine_g, pages[0]));
+        fetch_v(group_at(4 * t0 + mine_g, pages[0]));
     }
 
     // Queries: the lane's row, channels 16 ks + 8 half .. + 7.
@@ -623,35 +626,65 @@ __device__ __forceinline__ void wide_segment(const AttnArgs& a, const Sequence& 
         for (int v = 0; v < 16; ++v) o[c][v] = 0;
     float m = -INFINITY, l = 0;
 
+    // A step's products in their order: the next tile's scores (32 tokens s % 2, 16 channels s / 2) for s = 0, 1, .. and, from the first eight
+    // exponentials on, this tile's outputs between them.
+    struct Product {
+        bool score;
+        int i, k;  // score: half of the tile, channels; output: 16 tokens, tile of channels
+    };
+    constexpr int L = D / 16, kProducts = 2 * KS + 4 * CT, kAhead = 4;  // L products to 8 exponentials
+    constexpr auto product = [](int n) constexpr -> Product {
+        if (n < L) return {true, n % 2, n / 2};
+        if (n < 3 * L) {
+            const int g = n / L, r = n % L, s = L + (g - 1) * (L / 2) + r / 2;
+            return r % 2 ? Product{true, s % 2, s / 2} : Product{false, g - 1, r / 2};
+        }
+        return {false, 2 + (n - 3 * L) / CT, (n - 3 * L) % CT};
+    };
+    auto operand = [&](int n, int t) {
+        const Product p = product(n);
+        return p.score ? lds.k[(t + 1) & 1][(p.i * KS + p.k) * 64 + lane] : lds.v[t & 1][(p.i * CT + p.k) * 64 + lane];
+    };
+    const uint8_t* at_v = a.cache;  // the bytes whose keys were fetched last: the next values to fetch
+    f32x16 xs[2][2];  // scores of the tile and of the next
     if (t0 < t1) {
-        put(t0, page);
-        page = ahead;
-        fetch(group_at(4 * (t0 + 1) + mine_g, page));
-        ahead = page_of(4 * (t0 + 2) + mine_g);
+        put_k(t0);
+        put_v(t0, pages[0]);
+        fetch_k(group_at(4 * (t0 + 1) + mine_g, pages[1]));
+        fetch_v(group_at(4 * (t0 + 1) + mine_g, pages[1]));
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+#pragma unroll
+            for (int v = 0; v < 16; ++v) xs[0][i][v] = 0;
+#pragma unroll
+            for (int k = 0; k < KS; ++k)
+                xs[0][i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, lds.k[t0 & 1][(i * KS + k) * 64 + lane]), q[k], xs[0][i], 0, 0, 0);
+        }
+        put_k(t0 + 1);
+        at_v = group_at(4 * (t0 + 2) + mine_g, pages[2]);
+        fetch_k(at_v);
+        pages[0] = pages[1], pages[1] = pages[2], pages[2] = ahead;
+        ahead = page_of(4 * (t0 + 4) + mine_g);
     }
-    for (int t = t0; t < t1; ++t) {
-        __syncthreads();  // tile t is there, and nobody reads the other buffer any more
-        const int buf = t & 1;
-        const bool work = t * kWideTile < top_key;
-        f32x16 x[2];
-        if (work) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-#pragma unroll
-                for (int v = 0; v < 16; ++v) x[i][v] = 0;
-#pragma unroll
-                for (int k = 0; k < KS; ++k)
-                    x[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, lds.k[buf][(i * KS + k) * 64 + lane]), q[k], x[i], 0, 0, 0);
-            }
-        }
+    // One tile: its scores are in x, and the next one's go to y (behind the last: of whatever lies there, for nobody).
+    auto step = [&](int t, f32x16 (&x)[2], f32x16 (&y)[2]) {
+        __syncthreads();  // keys of tile t + 1 and values of tile t are there, and nobody reads keys of t or values of t - 1 any more
         if (t + 1 < t1) {
-            put(t + 1, page);
-            page = ahead;
-            fetch(group_at(4 * (t + 2) + mine_g, page));
-            ahead = page_of(4 * (t + 3) + mine_g);
+            put_v(t + 1, pages[0]);
+            put_k(t + 2);
+            fetch_v(at_v);
+            at_v = group_at(4 * (t + 3) + mine_g, pages[2]);
+            fetch_k(at_v);
+            pages[0] = pages[1], pages[1] = pages[2], pages[2] = ahead;
+            ahead = page_of(4 * (t + 5) + mine_g);
         }
-        if (!work) continue;
+        if (t * kWideTile >= top_key) return;
+        const int buf = t & 1;
         const uint4 flags = *(const uint4*)lds.flags[buf];
+        uint4 op[kAhead];
+#pragma unroll
+        for (int n = 0; n < kAhead; ++n) op[n] = operand(n, t);
         const unsigned any = __builtin_amdgcn_readfirstlane(flags.x | flags.y | flags.z | flags.w);
         if ((t + 1) * kWideTile > least) {
             const int seen = limit - t * kWideTile - 4 * (int)half;
@@ -687,21 +720,33 @@ __device__ __forceinline__ void wide_segment(const AttnArgs& a, const Sequence& 
             for (int c = 0; c < CT; ++c) o[c] *= by;
         }
         const float ref = m == -INFINITY ? 0.f : m;
+        f16x8 p[4];
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                f16x8 p;
+            for (int v = 0; v < 16; ++v) y[i][v] = 0;
+        auto multiply = [&](int n) {
+            const Product w = product(n);
+            const f16x8 f = __builtin_bit_cast(f16x8, op[n % kAhead]);
+            if (w.score) y[w.i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f, q[w.k], y[w.i], 0, 0, 0);
+            else o[w.k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f, p[w.i], o[w.k], 0, 0, 0);
+            if (n + kAhead < kProducts) op[n % kAhead] = operand(n + kAhead, t);
+        };
+        int n = 0;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float e = __builtin_amdgcn_exp2f(fmaf(x[i][8 * k + j], factor, -ref));
-                    l += e;
-                    p[j] = (_Float16)e;
-                }
+        for (int j = 0; j < 32; ++j) {
+            if (j * L / 8 * 8 == j * L && (j < 24 || j * L / 8 % 2 == 0)) multiply(n++);
+            const float e = __builtin_amdgcn_exp2f(fmaf(x[j / 16][j % 16], factor, -ref));
+            l += e;
+            p[j / 8][j % 8] = (_Float16)e;
+        }
 #pragma unroll
-                for (int c = 0; c < CT; ++c)
-                    o[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, lds.v[buf][((2 * i + k) * CT + c) * 64 + lane]), p, o[c], 0, 0, 0);
-            }
+        for (int i = 0; i < CT; ++i) multiply(n++);
+    };
+    for (int t = t0; t < t1; ++t) {
+        step(t, xs[0], xs[1]);
+        if (++t >= t1) break;
+        step(t, xs[1], xs[0]);
     }
 
     l += __shfl_xor(l, 32);
@@ -748,7 +793,7 @@ struct Narrow {
 };
 template <int D, int NW, bool BF>
 struct Wide {
-    static constexpr int rows = 32 * NW, tile = kWideTile, waves_simd = D == 64 ? 3 : 2, threads = 64 * NW;
+    static constexpr int rows = 32 * NW, tile = kWideTile, waves_simd = 2, threads = 64 * NW;
     static constexpr int begin = 2, least = 4, whole = 32;
     typedef WideShared<D> Lds;
     template <class... A>
@@ -905,8 +950,12 @@ struct Choice {
 //  * kRanges: 768, 1024, 1536, 2048 ranges: 64 sequences of up to 8192 keys 83, 80, 83, 82; two of up to 131072 40, 42, 47, 49.  Eight waves a workgroup
 //    and half the ranges: 87 and 40.
 //    Forms of which two workgroups fill a unit, 1024 and 512: 24 rows over 16 caches of up to 6000 keys 34, 26, the same of 32 rows, d = 64, 26, 21.5.
+//  * kMany: 256 rows a workgroup instead of 128 halve the conversions, but twice as many rows begin and end together: 2048 queries behind 14336 keys
+//    497 against 475, 300 behind 12000, 16 heads on 4, d = 64, 62 against 59 (1200 rows), 150 behind 12000 82 against 83.5 (600 rows); caches of 2048 keys, which
+//    are not cut, 52 against 61.
 //  * kShort: caches of 1500 keys cut all the same: 64 sequences 23 against 20, one of 1003 keys 11.7 against 10.9 with its 16 waves, prompts 39 against 31.
 constexpr int kShort = 2048;   // keys up to which nothing is cut
+constexpr int kMany = 1024;    // rows of a sequence and head from which 256 of them share a tile's conversion
 constexpr int kRanges = 1024;  // four workgroups of 128 registers on each of 256 units; of the other forms two, and half the ranges
 
 Choice choose(long long T, int B, int H, int heads, int d, long long cap, int max_q) {
@@ -914,9 +963,9 @@ Choice choose(long long T, int B, int H, int heads, int d, long long cap, int ma
     Choice c;
     c.wide = rows > 32;
     c.nt = rows <= 16 ? 1 : 2;
-    c.nw = 4;
-    c.rows = c.wide ? 128 : 16 * c.nt;
-    c.target = c.wide || c.nt == 2 ? kRanges / 2 : kRanges;
+    c.nw = c.wide && cap > kShort && rows >= kMany ? 8 : 4;
+    c.rows = c.wide ? 32 * c.nw : 16 * c.nt;
+    c.target = c.nw == 8 ? kRanges / 4 : c.wide || c.nt == 2 ? kRanges / 2 : kRanges;
     const long long alone = c.segments = B * ((rows + c.rows - 1) / c.rows) * heads;
     // Segments that fill the launch by themselves stay whole, and so do those that cannot be long: if they are few, 16 waves take one,
     // up to four tiles each.
@@ -942,7 +991,8 @@ int check_sizes(long long T, int B, int H, int heads, int d, int page_size, int 
 
 template <int D, bool BF>
 int launch_attn(const Choice& c, AttnArgs& a, void* stream) {
-    const void* fn = c.wide      ? (const void*)attn_kernel<Wide<D, 4, BF>>
+    const void* fn = c.nw == 8   ? (const void*)attn_kernel<Wide<D, 8, BF>>
+                     : c.wide    ? (const void*)attn_kernel<Wide<D, 4, BF>>
                      : c.nw == 16 ? (const void*)attn_kernel<Narrow<D, 1, 16, BF>>
                      : c.nt == 1  ? (const void*)attn_kernel<Narrow<D, 1, 4, BF>>
                                   : (const void*)attn_kernel<Narrow<D, 2, 4, BF>>;
@@ -955,7 +1005,8 @@ int launch_attn(const Choice& c, AttnArgs& a, void* stream) {
     };
     const void* join = c.rows == 16   ? join_of(std::integral_constant<int, 16>())
                        : c.rows == 32 ? join_of(std::integral_constant<int, 32>())
-                                      : join_of(std::integral_constant<int, 128>());
+                       : c.rows == 128 ? join_of(std::integral_constant<int, 128>())
+                                       : join_of(std::integral_constant<int, 256>());
     void* list[] = {&a};
     if (hipLaunchKernel(fn, dim3((unsigned)c.blocks), dim3(64 * c.nw), list, 0, (hipStream_t)stream) != hipSuccess ||
         (a.ws && hipLaunchKernel(join, dim3((unsigned)(waves == 1 ? (rows + 3) / 4 : rows)), dim3(waves == 16 ? 1024 : 256), list, 0, (hipStream_t)stream) != hipSuccess)) {

@@ -424,3 +424,34 @@ def test_a_layer_from_projection_to_attention(dtype):
     # one causal pass over all tokens and the cache as it is now
     want = R.attention(f64(torch.cat(qs)), R.values(cache.cpu().numpy()), table.cpu().numpy(), [n + later], [0, n + later], True, d ** -0.5)
     check(torch.cat([o for o, _ in outs]), torch.cat([l for _, l in outs]), want, dtype, scores=60)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("case", [([3000, 40, 0, 2500], [300, 30, 5, 256], 8, 2, 64, 16, True), ([2300, 2100], [257, 3], 8, 1, 128, 32, True),
+                                  ([2500], [270], 4, 1, 128, 64, False)], ids=["four", "two", "all keys"])
+def test_many_rows_over_long_caches(case, dtype):
+    """More than a thousand rows to a sequence and head: blocks of 256 rows, cut and not, and pages that are not there."""
+    s = setup(case, dtype)
+    s["tables"][0, 3] = -1
+    want = reference(s)
+    check(*run(s), want, dtype, scores=60)
+    uncut = run(s, stream=torch.cuda.Stream().cuda_stream)
+    torch.cuda.synchronize()
+    check(*uncut, want, dtype, scores=60)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_nan_in_a_long_cache_of_many_rows(d):
+    n, nq, key = 2200, 600, 2130
+    s = setup(([n], [nq], 2, 1, d, 16, True), torch.float16)
+    cache = s["cache"].cpu().numpy()
+    want = reference(s)
+    for what in (4, 3):                                            # the scale of a value block, then of a key block
+        bad = cache.copy()
+        bad[int(s["tables"][0, key // 16]), 0].reshape(-1)[R.token_place(d, key % 16, 33)[what]] = 255
+        s["cache"] = torch.from_numpy(bad).cuda()
+        out, lse = run(s)
+        seen = np.array([key <= n - nq + i for i in range(nq)])
+        check(out, lse, want, torch.float16, scores=60, rows=~seen)
+        got = f64(out)[seen]
+        assert np.isnan(got[..., 32:64]).all() and (what == 4 or (np.isnan(got).all() and np.isnan(f64(lse)[seen]).all()))
