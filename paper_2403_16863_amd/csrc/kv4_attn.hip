@@ -209,12 +209,12 @@ __device__ __forceinline__ void segment(const AttnArgs& a, const Sequence& s, in
 
     const const_ints table = (const_ints)(uintptr_t)(a.tables + (long long)b * a.width);
     const int groups_page = 1 << (a.page_shift - 4);
-    // Group g's (16 tokens') page; groups behind the last one stand for that one (their keys are masked).
+    // Group g's (16 tokens') page; groups behind the last one stand for that one (their keys are masked).  All groups are fewer than 2^32.
     const int last_group = max(0, (most + 15) / 16 - 1);
     auto page_of = [&](int g) { return table[min(g, last_group) >> (a.page_shift - 4)]; };
     auto group_at = [&](int g, int page) {
         const int p = (unsigned)page < (unsigned)a.pages ? page : 0;
-        return a.cache + (((long long)p * a.heads + h) * groups_page + (min(g, last_group) & (groups_page - 1))) * Group<D>::bytes;
+        return a.cache + (unsigned long long)(((unsigned)p * a.heads + h) * groups_page + (min(g, last_group) & (groups_page - 1))) * Group<D>::bytes;
     };
     // A lane's places in a group, unsigned so that they are 32-bit offsets to a scalar address.
     const unsigned k_off = col * (D / 2) + quad * (D / 8), ks_off = Group<D>::k_scales + col * (D / 32) + quad * (D / 4) / 32;
@@ -495,7 +495,7 @@ __device__ __forceinline__ void wide_segment(const AttnArgs& a, const Sequence& 
     auto page_of = [&](int g) { return table[min(g, last_group) >> (a.page_shift - 4)]; };
     auto group_at = [&](int g, int page) {
         const int p = (unsigned)page < (unsigned)a.pages ? page : 0;
-        return a.cache + (((long long)p * a.heads + h) * groups_page + (min(g, last_group) & (groups_page - 1))) * Group<D>::bytes;
+        return a.cache + (unsigned long long)(((unsigned)p * a.heads + h) * groups_page + (min(g, last_group) & (groups_page - 1))) * Group<D>::bytes;
     };
     // Groups of 16 tokens are shared out: with eight waves four convert keys and four values, with four a wave does both of its group.
     const int mine_g = wave & 3;
@@ -670,6 +670,11 @@ __device__ __forceinline__ void wide_segment(const AttnArgs& a, const Sequence& 
     // One tile: its scores are in x, and the next one's go to y (behind the last: of whatever lies there, for nobody).
     auto step = [&](int t, f32x16 (&x)[2], f32x16 (&y)[2]) {
         __syncthreads();  // keys of tile t + 1 and values of tile t are there, and nobody reads keys of t or values of t - 1 any more
+        const int buf = t & 1;
+        const uint4 flags = *(const uint4*)lds.flags[buf];
+        uint4 op[kAhead];
+#pragma unroll
+        for (int n = 0; n < kAhead; ++n) op[n] = operand(n, t);
         if (t + 1 < t1) {
             put_v(t + 1, pages[0]);
             put_k(t + 2);
@@ -680,12 +685,6 @@ __device__ __forceinline__ void wide_segment(const AttnArgs& a, const Sequence& 
             ahead = page_of(4 * (t + 5) + mine_g);
         }
         if (t * kWideTile >= top_key) return;
-        const int buf = t & 1;
-        const uint4 flags = *(const uint4*)lds.flags[buf];
-        uint4 op[kAhead];
-#pragma unroll
-        for (int n = 0; n < kAhead; ++n) op[n] = operand(n, t);
-        const unsigned any = __builtin_amdgcn_readfirstlane(flags.x | flags.y | flags.z | flags.w);
         if ((t + 1) * kWideTile > least) {
             const int seen = limit - t * kWideTile - 4 * (int)half;
 #pragma unroll
@@ -693,6 +692,16 @@ __device__ __forceinline__ void wide_segment(const AttnArgs& a, const Sequence& 
 #pragma unroll
                 for (int v = 0; v < 16; ++v) x[i][v] = 32 * i + 8 * (v / 4) + v % 4 < seen ? x[i][v] : -INFINITY;
         }
+        auto largest = [&] {
+            float top = x[0][0];
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) top = fmaxf(top, x[i][v]);
+            return top;
+        };
+        float top = largest();
+        const unsigned any = __builtin_amdgcn_readfirstlane(flags.x | flags.y | flags.z | flags.w);
         if (__builtin_expect(any != 0, 0)) {
 #pragma unroll
             for (int i = 0; i < 2; ++i)
@@ -703,12 +712,8 @@ __device__ __forceinline__ void wide_segment(const AttnArgs& a, const Sequence& 
                     const bool seen = t * kWideTile + 32 * i + in + 4 * (int)half < limit;
                     x[i][v] = f >> 16 ? -INFINITY : f >> (in % 16 + 4 * half) & 1 && seen ? __uint_as_float(0x7fc00000u) : x[i][v];
                 }
+            top = largest();
         }
-        float top = x[0][0];
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) top = fmaxf(top, x[i][v]);
         top *= factor;
         if (__any(top > m + kRaise)) {
             top = fmaxf(top, __shfl_xor(top, 32));
@@ -1035,7 +1040,7 @@ int kv4_attn(const void* q, const void* cache, const int* tables, const int* len
     if (T == 0 && B >= 1) return KV4_OK;
     if (!cu_q && (B < 1 || T % B || max_q != T / B)) return KV4_EINVAL;
     if (const int rc = check_sizes(T, B, H, heads, d, page_size, width, max_q)) return rc;
-    if ((long long)pages * page_size > INT_MAX) return KV4_EUNSUPPORTED;
+    if ((long long)pages * page_size > INT_MAX || (long long)pages * heads * (page_size / 16) > UINT_MAX) return KV4_EUNSUPPORTED;
     const long long bytes = (long long)T * H * d * 2;
     const long long held = (long long)pages * heads * page_size * (d + d / 16);
     if (overlap(q, bytes, out, bytes) || overlap(lse, (long long)T * H * 4, out, bytes) || overlap(cache, held, out, bytes)) return KV4_EINVAL;

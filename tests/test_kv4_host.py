@@ -152,3 +152,13 @@ def test_sizes_at_the_limits_of_32_bits():
         cache, q = z(3, 2, 16, 68, dtype=torch.uint8), z(0, 4, 64)
         kv4.kv4_attn(q, cache, z(0, 5, dtype=i32), z(0, dtype=i32), q, z(0, 4, dtype=f32), True, 1.0)
         kv4.kv4_attn(q, cache, z(2, 5, dtype=i32), z(2, dtype=i32), q, z(0, 4, dtype=f32), True, 1.0)
+
+
+def test_attention_refuses_caches_of_too_many_groups():
+    L = kv4.lib()
+
+    def call(pages, heads, cache=0x200000):
+        return L.kv4_attn(p(0x100000), p(cache), p(0x300000), p(0x400000), p(0x500000), p(0x600000), p(0x700000), 4, 2, heads, heads, 64, pages, 16,
+                          5, 3, 1, 0.1, 0, None, 0, None)
+    assert call(1 << 26, 64) == kv4.KV4_EUNSUPPORTED               # 2^32 groups of 16 tokens
+    assert call((1 << 27) - 1, 32) == kv4.KV4_EINVAL               # fewer, but out within them
