@@ -468,20 +468,27 @@ __device__ __forceinline__ void segment(const AttnArgs& a, const Sequence& s, in
 // exponentials run, the next one's scores are multiplied between them (one after the other: 2048 queries behind as many keys 55 us, so 52).
 //     S^T (32 tokens x 32 rows) = K Q^T:  lane l has row l % 32 of Q, register v token 8 (v / 4) + 4 (l / 32) + v % 4
 //     O^T (32 channels x 32 rows) += V^T P^T: P as S^T leaves it, so half l / 32 has tokens 4 (l / 32) .. + 3 and 8 + 4 (l / 32) .. + 3 of 16
-// A row's output stays in one wave: nothing to join within the workgroup.
+// A row's output stays in one wave (of each group).
 constexpr int kWideTile = 64;
 
 template <int D>
-struct WideShared {
+struct WideTiles {
     uint4 k[2][2 * (D / 16) * 64], v[2][4 * (D / 32) * 64];  // [buffer][32 tokens][16 channels][lane], [buffer][16 tokens][32 channels][lane]
     unsigned flags[2][4];  // of 16 tokens: whose values hold a NaN, and (bit 16) whether their page is outside the cache
 };
+template <int D, int G>
+struct WideShared {
+    WideTiles<D> of[G];
+};
 
-template <int D, int NW, bool BF>
+// G = 2: two groups of NW waves take turns at the tiles of the same rows, whole segments only.
+template <int D, int NW, int G, bool BF>
 __device__ __forceinline__ void wide_segment(const AttnArgs& a, const Sequence& s, int b, int h, int rb, int t0, int t1, int most, int pieces,
-                                             int slot, WideShared<D>& lds) {
+                                             int slot, WideShared<D, G>& shared) {
     constexpr int RB = 32 * NW, KS = D / 16, CT = D / 32, W = D / 32, RUN = D / 16;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) % NW);
+    const int turn = __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) / NW);
+    WideTiles<D>& lds = shared.of[turn];
     const unsigned col = lane & 31, half = lane >> 5, c16 = lane & 15, quad = lane >> 4;
     const int rows = s.nq * a.group, row0 = rb * RB + 32 * wave, row = row0 + (int)col;
     const bool first = t0 == 0, mine = row < rows;
@@ -519,7 +526,7 @@ __device__ __forceinline__ void wide_segment(const AttnArgs& a, const Sequence& 
     };
     auto put_k = [&](int t) {  // the lane's token and D/4 channels from quad * D/4
         if (!keys) return;
-        uint4* to = lds.k[t & 1] + ((mine_g >> 1) * KS * 64 + (mine_g & 1) * 16 + c16);
+        uint4* to = lds.k[t / G & 1] + ((mine_g >> 1) * KS * 64 + (mine_g & 1) * 16 + c16);
 #pragma unroll
         for (int w = 0; w < W; ++w) {
             const unsigned piece = quad * W + w;  // 8 channels: half piece % 2 of 16
@@ -528,7 +535,7 @@ __device__ __forceinline__ void wide_segment(const AttnArgs& a, const Sequence& 
     };
     auto put_v = [&](int t, int page) {
         if (!vals) return;
-        const int buf = t & 1, key = t * kWideTile + 16 * mine_g + 4 * (int)quad;
+        const int buf = t / G & 1, key = t * kWideTile + 16 * mine_g + 4 * (int)quad;
         const bool there = (unsigned)page < (unsigned)a.pages;
         if (!there || t * kWideTile + 16 * mine_g + 16 > most) {
             const int live = there ? most - key : 0;
@@ -578,13 +585,14 @@ __device__ __forceinline__ void wide_segment(const AttnArgs& a, const Sequence& 
         }
     };
 
-    int pages[3] = {-1, -1, -1};  // of the wave's groups in the tiles t + 1, t + 2 and t + 3
+    const int t00 = t0 + turn;
+    int pages[3] = {-1, -1, -1};  // of the wave's tokens in the tiles t + G, t + 2 G and t + 3 G
     int ahead = -1;
     if (t0 < t1) {
-        for (int i = 0; i < 3; ++i) pages[i] = page_of(4 * (t0 + i) + mine_g);
-        ahead = page_of(4 * (t0 + 3) + mine_g);
-        fetch_k(group_at(4 * t0 + mine_g, pages[0]));
-        fetch_v(group_at(4 * t0 + mine_g, pages[0]));
+        for (int i = 0; i < 3; ++i) pages[i] = page_of(4 * (t00 + G * i) + mine_g);
+        ahead = page_of(4 * (t00 + 3 * G) + mine_g);
+        fetch_k(group_at(4 * t00 + mine_g, pages[0]));
+        fetch_v(group_at(4 * t00 + mine_g, pages[0]));
     }
 
     // Queries: the lane's row, channels 16 ks + 8 half .. + 7.
@@ -643,15 +651,15 @@ __device__ __forceinline__ void wide_segment(const AttnArgs& a, const Sequence& 
     };
     auto operand = [&](int n, int t) {
         const Product p = product(n);
-        return p.score ? lds.k[(t + 1) & 1][(p.i * KS + p.k) * 64 + lane] : lds.v[t & 1][(p.i * CT + p.k) * 64 + lane];
+        return p.score ? lds.k[(t / G + 1) & 1][(p.i * KS + p.k) * 64 + lane] : lds.v[t / G & 1][(p.i * CT + p.k) * 64 + lane];
     };
     const uint8_t* at_v = a.cache;  // the bytes whose keys were fetched last: the next values to fetch
     f32x16 xs[2][2];  // scores of the tile and of the next
     if (t0 < t1) {
-        put_k(t0);
-        put_v(t0, pages[0]);
-        fetch_k(group_at(4 * (t0 + 1) + mine_g, pages[1]));
-        fetch_v(group_at(4 * (t0 + 1) + mine_g, pages[1]));
+        put_k(t00);
+        put_v(t00, pages[0]);
+        fetch_k(group_at(4 * (t00 + G) + mine_g, pages[1]));
+        fetch_v(group_at(4 * (t00 + G) + mine_g, pages[1]));
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -659,30 +667,30 @@ __device__ __forceinline__ void wide_segment(const AttnArgs& a, const Sequence& 
             for (int v = 0; v < 16; ++v) xs[0][i][v] = 0;
 #pragma unroll
             for (int k = 0; k < KS; ++k)
-                xs[0][i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, lds.k[t0 & 1][(i * KS + k) * 64 + lane]), q[k], xs[0][i], 0, 0, 0);
+                xs[0][i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, lds.k[t00 / G & 1][(i * KS + k) * 64 + lane]), q[k], xs[0][i], 0, 0, 0);
         }
-        put_k(t0 + 1);
-        at_v = group_at(4 * (t0 + 2) + mine_g, pages[2]);
+        put_k(t00 + G);
+        at_v = group_at(4 * (t00 + 2 * G) + mine_g, pages[2]);
         fetch_k(at_v);
         pages[0] = pages[1], pages[1] = pages[2], pages[2] = ahead;
-        ahead = page_of(4 * (t0 + 4) + mine_g);
+        ahead = page_of(4 * (t00 + 4 * G) + mine_g);
     }
     // One tile: its scores are in x, and the next one's go to y (behind the last: of whatever lies there, for nobody).
     auto step = [&](int t, f32x16 (&x)[2], f32x16 (&y)[2]) {
-        __syncthreads();  // keys of tile t + 1 and values of tile t are there, and nobody reads keys of t or values of t - 1 any more
-        const int buf = t & 1;
+        __syncthreads();  // keys of tile t + G and values of tile t are there, and nobody reads keys of t or values of t - G any more
+        const int buf = t / G & 1;
         const uint4 flags = *(const uint4*)lds.flags[buf];
         uint4 op[kAhead];
 #pragma unroll
         for (int n = 0; n < kAhead; ++n) op[n] = operand(n, t);
-        if (t + 1 < t1) {
-            put_v(t + 1, pages[0]);
-            put_k(t + 2);
+        if (t + G < t1) {
+            put_v(t + G, pages[0]);
+            put_k(t + 2 * G);
             fetch_v(at_v);
-            at_v = group_at(4 * (t + 3) + mine_g, pages[2]);
+            at_v = group_at(4 * (t + 3 * G) + mine_g, pages[2]);
             fetch_k(at_v);
             pages[0] = pages[1], pages[1] = pages[2], pages[2] = ahead;
-            ahead = page_of(4 * (t + 5) + mine_g);
+            ahead = page_of(4 * (t + 5 * G) + mine_g);
         }
         if (t * kWideTile >= top_key) return;
         if ((t + 1) * kWideTile > least) {
@@ -748,13 +756,36 @@ __device__ __forceinline__ void wide_segment(const AttnArgs& a, const Sequence& 
 #pragma unroll
         for (int i = 0; i < CT; ++i) multiply(n++);
     };
-    for (int t = t0; t < t1; ++t) {
+    for (int t = t00; t - turn < t1; t += G) {  // as many steps in both groups: behind t1 nobody has a key
         step(t, xs[0], xs[1]);
-        if (++t >= t1) break;
+        if ((t += G) - turn >= t1) break;
         step(t, xs[1], xs[0]);
     }
 
     l += __shfl_xor(l, 32);
+    if constexpr (G == 2) {  // the second group's rows go to the first through LDS
+        constexpr int n = 16 * CT + 2;
+        static_assert(sizeof(shared) >= NW * n * 64 * sizeof(float), "room for the rows of a group");
+        float* const at = (float*)&shared + wave * n * 64 + lane;
+        __syncthreads();
+        if (turn) {
+#pragma unroll
+            for (int c = 0; c < CT; ++c)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) at[(16 * c + v) * 64] = o[c][v];
+            at[(n - 2) * 64] = m, at[(n - 1) * 64] = l;
+        }
+        __syncthreads();
+        if (turn) return;
+        const float other = at[(n - 2) * 64], top = fmaxf(m, other), ref = top == -INFINITY ? 0.f : top;
+        const float by = __builtin_amdgcn_exp2f(m - ref), add = __builtin_amdgcn_exp2f(other - ref);
+        m = top;
+        l = l * by + at[(n - 1) * 64] * add;
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) o[c][v] = o[c][v] * by + at[(16 * c + v) * 64] * add;
+    }
     if (!mine) return;
     const long long vec = (long long)(s.q0 + row / a.group) * a.H + h * a.group + row % a.group;
     const int at = slot * RB + 32 * wave + (int)col;
@@ -785,7 +816,7 @@ __device__ __forceinline__ void wide_segment(const AttnArgs& a, const Sequence& 
         }
 }
 
-// The two forms of a segment: NT tiles of 16 rows with the keys shared out to NW waves, or 32 rows to each of NW waves.  In tiles: `begin`, what
+// The two forms of a segment: NT tiles of 16 rows with the keys shared out to NW waves, or 32 rows to each of NW waves in G groups.  In tiles: `begin`, what
 // it costs a workgroup to begin and end a segment (about 5 us; 0, 4, 8, 16 tiles: 64 sequences of up to 8192 keys 80, 76, 74.5, 74.3 us, 8 of up to
 // 4000 19.2, 16.6, 15.5, 15.4); `least`, the shortest range; `whole`, up to which a segment is left whole if no other is longer.
 template <int D, int NT, int NW, bool BF>
@@ -796,13 +827,13 @@ struct Narrow {
     template <class... A>
     static __device__ __forceinline__ void run(A&&... x) { segment<D, NT, NW, BF>(x...); }
 };
-template <int D, int NW, bool BF>
+template <int D, int NW, int G, bool BF>
 struct Wide {
-    static constexpr int rows = 32 * NW, tile = kWideTile, waves_simd = 2, threads = 64 * NW;
+    static constexpr int rows = 32 * NW, tile = kWideTile, waves_simd = 2, threads = 64 * NW * G;
     static constexpr int begin = 2, least = 4, whole = 32;
-    typedef WideShared<D> Lds;
+    typedef WideShared<D, G> Lds;
     template <class... A>
-    static __device__ __forceinline__ void run(A&&... x) { wide_segment<D, NW, BF>(x...); }
+    static __device__ __forceinline__ void run(A&&... x) { wide_segment<D, NW, G, BF>(x...); }
 };
 
 template <class F>
@@ -945,7 +976,7 @@ __global__ __launch_bounds__(WAVES > 4 ? 64 * WAVES : 256) void join_kernel(Attn
 }
 
 struct Choice {
-    int wide, nt, nw, rows, target;  // wide: 32 rows a wave; otherwise nt tiles of 16 rows
+    int wide, nt, nw, groups, rows, target;  // wide: 32 rows a wave, `groups` of nw waves; otherwise nt tiles of 16 rows
     long long segments, blocks, slots, bytes;
 };
 
@@ -958,9 +989,12 @@ struct Choice {
 //  * kMany: 256 rows a workgroup instead of 128 halve the conversions, but twice as many rows begin and end together: 2048 queries behind 14336 keys
 //    497 against 475, 300 behind 12000, 16 heads on 4, d = 64, 62 against 59 (1200 rows), 150 behind 12000 82 against 83.5 (600 rows); caches of 2048 keys, which
 //    are not cut, 52 against 61.
+//  * kPaired: one prompt of 1500, 12 heads on 4, d = 64, 22.3 against 26.2, eight times 100 queries over 2000 keys 37 against 43 (256 row blocks), three prompts of
+//    1500 (432) 29.1 against 28.6, two of 32 heads (752) 65 against 53.  Of 200 keys, four tiles, 11.5 against 10.4: from 512 on.
 //  * kShort: caches of 1500 keys cut all the same: 64 sequences 23 against 20, one of 1003 keys 11.7 against 10.9 with its 16 waves, prompts 39 against 31.
 constexpr int kShort = 2048;   // keys up to which nothing is cut
 constexpr int kMany = 1024;    // rows of a sequence and head from which 256 of them share a tile's conversion
+constexpr int kPaired = 256;   // row blocks up to which two groups of waves share one: a workgroup to each unit
 constexpr int kRanges = 1024;  // four workgroups of 128 registers on each of 256 units; of the other forms two, and half the ranges
 
 Choice choose(long long T, int B, int H, int heads, int d, long long cap, int max_q) {
@@ -977,6 +1011,7 @@ Choice choose(long long T, int B, int H, int heads, int d, long long cap, int ma
     // The joining kernel has up to 16 waves for each row of q, somebody's or not, and threads of a launch are counted in 32 bits.
     const bool whole = cap <= kShort || alone >= 4 * c.target || T * H >= 1 << 22;
     if (c.nt == 1 && cap <= kShort && alone <= 256) c.nw = 16;
+    c.groups = c.wide && cap <= kShort && cap >= 512 && alone <= kPaired ? 2 : 1;
     c.blocks = whole || alone > c.target ? alone : c.target;
     c.slots = 2 * c.target;
     c.bytes = whole ? 0 : (T * H * 8 + 15) / 16 * 16 + c.slots * c.rows * (d + 2) * 4;
@@ -996,8 +1031,9 @@ int check_sizes(long long T, int B, int H, int heads, int d, int page_size, int 
 
 template <int D, bool BF>
 int launch_attn(const Choice& c, AttnArgs& a, void* stream) {
-    const void* fn = c.nw == 8   ? (const void*)attn_kernel<Wide<D, 8, BF>>
-                     : c.wide    ? (const void*)attn_kernel<Wide<D, 4, BF>>
+    const void* fn = c.nw == 8   ? (const void*)attn_kernel<Wide<D, 8, 1, BF>>
+                     : c.groups == 2 ? (const void*)attn_kernel<Wide<D, 4, 2, BF>>
+                     : c.wide    ? (const void*)attn_kernel<Wide<D, 4, 1, BF>>
                      : c.nw == 16 ? (const void*)attn_kernel<Narrow<D, 1, 16, BF>>
                      : c.nt == 1  ? (const void*)attn_kernel<Narrow<D, 1, 4, BF>>
                                   : (const void*)attn_kernel<Narrow<D, 2, 4, BF>>;
@@ -1013,7 +1049,7 @@ int launch_attn(const Choice& c, AttnArgs& a, void* stream) {
                        : c.rows == 128 ? join_of(std::integral_constant<int, 128>())
                                        : join_of(std::integral_constant<int, 256>());
     void* list[] = {&a};
-    if (hipLaunchKernel(fn, dim3((unsigned)c.blocks), dim3(64 * c.nw), list, 0, (hipStream_t)stream) != hipSuccess ||
+    if (hipLaunchKernel(fn, dim3((unsigned)c.blocks), dim3(64 * c.nw * c.groups), list, 0, (hipStream_t)stream) != hipSuccess ||
         (a.ws && hipLaunchKernel(join, dim3((unsigned)(waves == 1 ? (rows + 3) / 4 : rows)), dim3(waves == 16 ? 1024 : 256), list, 0, (hipStream_t)stream) != hipSuccess)) {
         (void)hipGetLastError();
         return KV4_ELAUNCH;

@@ -455,3 +455,24 @@ def test_nan_in_a_long_cache_of_many_rows(d):
         check(out, lse, want, torch.float16, scores=60, rows=~seen)
         got = f64(out)[seen]
         assert np.isnan(got[..., 32:64]).all() and (what == 4 or (np.isnan(got).all() and np.isnan(f64(lse)[seen]).all()))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_two_groups_of_waves_to_a_row_block(d):
+    """A few prompts of odd and even numbers of tiles, pages that are not there, and a NaN in either group's tiles."""
+    s = setup(([700, 64, 129, 1, 900], [100, 64, 50, 7, 60], 4, 2, d, 16, True), torch.bfloat16)
+    s["tables"][4, 5] = -1
+    check(*run(s), reference(s), torch.bfloat16, scores=60)
+    n, nq = 700, 100
+    s = setup(([n], [nq], 2, 1, d, 16, True), torch.float16)
+    cache = s["cache"].cpu().numpy()
+    want = reference(s)
+    for what, key in ((4, 630), (4, 650), (3, 630), (3, 650)):     # of a value block, then of a key block, in tiles 9 and 10
+        bad = cache.copy()
+        bad[int(s["tables"][0, key // 16]), 0].reshape(-1)[R.token_place(d, key % 16, 33)[what]] = 255
+        s["cache"] = torch.from_numpy(bad).cuda()
+        out, lse = run(s)
+        seen = np.array([key <= n - nq + i for i in range(nq)])
+        check(out, lse, want, torch.float16, scores=60, rows=~seen)
+        got = f64(out)[seen]
+        assert np.isnan(got[..., 32:64]).all() and (what == 4 or (np.isnan(got).all() and np.isnan(f64(lse)[seen]).all()))
