@@ -76,7 +76,7 @@ int kv4_read(const void* cache, const int* slots, void* k, void* v, int T, int h
  *           kernels have run; null or fewer bytes: each workgroup goes over all keys of its rows, which is slower for few
  *           long sequences or unequal ones.
  *  Limits (KV4_EUNSUPPORTED): pages * page_size <= 2^31 - 1, pages * heads * page_size < 2^36, width * page_size <= 2^31 - 2^16, T * H <= 2^31 - 1, H / heads * max_q <= 2^30,
- *           B <= 65535, fewer than 2^23 workgroups (16 to 128 rows of a sequence and head each), and these times width * page_size / 32 below 2^31 where
+ *           B <= 65535, fewer than 2^23 workgroups (16 to 256 rows of a sequence and head each), and these times width * page_size / 32 below 2^31 where
  *           there is a use for a workspace.
  *
  * Accuracy: products of 16-bit values (bfloat16 queries become binary16 relative to the row's largest) and of the cache's values in fp32, the probabilities
