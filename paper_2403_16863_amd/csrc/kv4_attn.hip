@@ -52,7 +52,10 @@ struct AttnArgs {
 };
 
 constexpr int kTile = 32;    // keys of a step of one wave
-constexpr float kRaise = 8;  // scores (in powers of two) by which a row may pass its reference before that is raised: P < 2^8 in binary16
+// A row's reference lies kRoom powers of two below its largest score when it was last raised, and is raised when a score passes it by more than
+// kRaise: P, in binary16, is 2^7 for the largest key and below 2^15 for any, so that what is rounded in steps of 2^-24 (P below 2^-14) is 21 powers of
+// two below the largest key's (with kRoom = 0, 14: many keys that far below a few could lose all they add up to).
+constexpr float kRaise = 15, kRoom = 7;
 
 struct Sequence {
     int len, q0, nq;
@@ -363,7 +366,7 @@ __device__ __forceinline__ void segment(const AttnArgs& a, const Sequence& s, in
             if (__any(top > m[n] + kRaise)) {  // all four lanes of a row take the same reference
                 top = fmaxf(top, __shfl_xor(top, 16));
                 top = fmaxf(top, __shfl_xor(top, 32));
-                const float to = fmaxf(m[n], top);
+                const float to = fmaxf(m[n], top - kRoom);
                 const float by = to == m[n] ? 1.f : __builtin_amdgcn_exp2f(m[n] - to);
                 m[n] = to;
                 l[n] *= by;
@@ -725,7 +728,7 @@ __device__ __forceinline__ void wide_segment(const AttnArgs& a, const Sequence& 
         top *= factor;
         if (__any(top > m + kRaise)) {
             top = fmaxf(top, __shfl_xor(top, 32));
-            const float to = fmaxf(m, top);
+            const float to = fmaxf(m, top - kRoom);
             const float by = to == m ? 1.f : __builtin_amdgcn_exp2f(m - to);
             m = to;
             l *= by;
