@@ -79,11 +79,13 @@ int kv4_read(const void* cache, const int* slots, void* k, void* v, int T, int h
  *           B <= 65535, fewer than 2^23 workgroups (16 to 256 rows of a sequence and head each), and these times width * page_size / 32 below 2^31 where
  *           there is a use for a workspace.
  *
- * Accuracy: products of 16-bit values (bfloat16 queries become binary16 relative to the row's largest) and of the cache's values in fp32, the probabilities
- * are rounded to binary16 before the second product, and out once at the end.  |out - exact| <= u |out| + 2^-11 sum_j p_j |v_j| +
- * 2^-32 sum_j |v_j| max_j p_j (binary16 has steps of 2^-24, and the largest p_j is taken as 2^7) + small fp32 terms, u = 2^-11 or 2^-8.  The order of all sums is fixed by the arguments and the contents of lens and cu_q: results do
+ * Accuracy: products of 16-bit values and of the cache's values in fp32 (bfloat16 queries become binary16 relative to the row's largest: elements
+ * below 2^-17 of it lose bits, below 2^-25 all), the probabilities are rounded to binary16 before the second product, and out once at the end.
+ * |out - exact| <= u |out| + 2^-11 sum_j p_j |v_j| + 2^-32 max_j p_j sum_j |v_j| + small fp32 terms, u = 2^-11 or 2^-8 (binary16 has steps of
+ * 2^-24, and the largest p_j is held as 2^7 or more).  The order of all sums is fixed by the arguments and the contents of lens and cu_q: results do
  * not change from run to run.
- * NaN: a query with a NaN or an infinity has NaN rows, and so has one that sees a key with a NaN.  A NaN among the values that a row
+ * NaN: a query with a NaN or an infinity has NaN rows, and so has one that sees a key with a NaN; rows with a score beyond 2^126, and bfloat16 rows whose largest
+ * element times |scale| passes 2^141, may be NaN.  A NaN among the values that a row
  * sees makes the 32 channels NaN that it stands in, and may make the whole row NaN; it never enters a row that does not see it. */
 int kv4_attn(const void* q, const void* cache, const int* tables, const int* lens, const int* cu_q, void* out, float* lse, int T,
              int B, int H, int heads, int d, int pages, int page_size, int width, int max_q, int causal, float scale, int dtype,

@@ -180,6 +180,25 @@ __device__ __forceinline__ int keys_of(const AttnArgs& a, const Sequence& s, int
     return a.causal ? max(0, s.len - s.nq + row / a.group + 1) : s.len;
 }
 
+// A row's scores are products of its queries, turned by the scale's sign (and zero: the largest score is found before the factor) and, in bfloat16, relative
+// to 2^e, times a factor.  `top` is the row's largest magnitude.  Where 2^e of the row would take the factor out of range, the queries stay 14 powers of two
+// larger; a factor below every normal number would make -infinity, a key that is not seen, a NaN, and no score that it makes differs from 0.
+struct Scale {
+    float factor, turn;
+    int e;
+};
+template <bool BF>
+__device__ __forceinline__ Scale scale_of(const AttnArgs& a, float top) {
+    Scale s = {a.scale_l2 == 0 ? 1.f : fabsf(a.scale_l2), a.scale_l2 < 0 ? -1.f : a.scale_l2 > 0 ? 1.f : 0.f, 0};
+    if (BF && top > 0 && top < INFINITY) {
+        s.e = ilogbf(top);
+        if (!(ldexpf(s.factor, s.e) < INFINITY)) s.e -= 14;
+        s.factor = ldexpf(s.factor, s.e);
+    }
+    s.factor = s.factor < INFINITY ? fmaxf(s.factor, 0x1p-126f) : __uint_as_float(0x7fc00000u);
+    return s;
+}
+
 // One tile's bytes of one lane: [group of 16 tokens][words].
 template <int D>
 struct Raw {
@@ -253,9 +272,6 @@ __device__ __forceinline__ void segment(const AttnArgs& a, const Sequence& s, in
         const bool there = row < rows;
         limit[n] = there ? keys_of(a, s, row) : 0;
         const long long at = ((long long)(s.q0 + (there ? row / a.group : 0)) * a.H + h * a.group + (there ? row % a.group : 0)) * D + quad * (D / 4);
-        factor[n] = fabsf(a.scale_l2);  // its sign goes to the queries, and zero too: the largest score is found before this factor
-        const float turn = a.scale_l2 < 0 ? -1.f : a.scale_l2 > 0 ? 1.f : 0.f;
-        if (turn == 0) factor[n] = 1;
         float x[KS][8], top = 0;
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
@@ -263,18 +279,17 @@ __device__ __forceinline__ void segment(const AttnArgs& a, const Sequence& s, in
 #pragma unroll
             for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[k][i]));
         }
-        int e = 0;
         if (BF) {
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
-            if (top > 0 && top < INFINITY) e = ilogbf(top);
-            factor[n] *= ldexpf(1.f, e);
         }
+        const Scale scale = scale_of<BF>(a, top);
+        factor[n] = scale.factor;
         if (top == INFINITY) x[0][0] = __uint_as_float(0x7fc00000u);  // an infinity among the scores would hide where all of them are -inf
 #pragma unroll
         for (int k = 0; k < KS; ++k)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) q[n][k][i] = (_Float16)(turn * (BF ? ldexpf(x[k][i], -e) : x[k][i]));
+            for (int i = 0; i < 8; ++i) q[n][k][i] = (_Float16)(scale.turn * (BF ? ldexpf(x[k][i], -scale.e) : x[k][i]));
     }
 
     f32x4 o[NT][CT];
@@ -600,10 +615,8 @@ __device__ __forceinline__ void wide_segment(const AttnArgs& a, const Sequence& 
 
     // Queries: the lane's row, channels 16 ks + 8 half .. + 7.
     f16x8 q[KS];
-    float factor = fabsf(a.scale_l2);  // as in `segment`
+    float factor;
     {
-        const float turn = a.scale_l2 < 0 ? -1.f : a.scale_l2 > 0 ? 1.f : 0.f;
-        if (turn == 0) factor = 1;
         const long long at = ((long long)(s.q0 + (mine ? row / a.group : 0)) * a.H + h * a.group + (mine ? row % a.group : 0)) * D + 8 * half;
         float top = 0;
         uint4 raw[KS];
@@ -615,19 +628,16 @@ __device__ __forceinline__ void wide_segment(const AttnArgs& a, const Sequence& 
 #pragma unroll
             for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[i]));
         }
-        int e = 0;
-        if (BF) {
-            top = fmaxf(top, __shfl_xor(top, 32));
-            if (top > 0 && top < INFINITY) e = ilogbf(top);
-            factor *= ldexpf(1.f, e);
-        }
+        if (BF) top = fmaxf(top, __shfl_xor(top, 32));
+        const Scale scale = scale_of<BF>(a, top);
+        factor = scale.factor;
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
             float x[8];
             values_of<BF>(raw[k], x);
             if (k == 0 && top == INFINITY) x[0] = __uint_as_float(0x7fc00000u);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) q[k][i] = (_Float16)(turn * (BF ? ldexpf(x[i], -e) : x[i]));
+            for (int i = 0; i < 8; ++i) q[k][i] = (_Float16)(scale.turn * (BF ? ldexpf(x[i], -scale.e) : x[i]));
         }
     }
     f32x16 o[CT];

@@ -74,3 +74,33 @@ def test_keys_far_below_the_largest_count(form, dtype, cut):
         tol = U[dtype] * np.abs(o) + (2.0 ** -11 + 2.0 ** -16) * spread + rest + 2.0 ** -24
         assert (np.abs(out - o) <= tol).all(), (nats, float((np.abs(out - o) / tol).max()))
         assert (np.abs(lse - l) <= 2.0 ** -19 * 26).all(), nats
+
+
+@pytest.mark.parametrize("cut", [True, False], ids=["cut", "uncut"])
+@pytest.mark.parametrize("form", FORMS)
+def test_scales_and_queries_whose_product_leaves_the_range_of_32_bits(form, cut):
+    n, rows, page = FORMS[form]
+    g = torch.Generator().manual_seed(rows)
+    k, v = torch.zeros(n, 64), torch.randn(n, 64, generator=g)
+    k[:, 32:] = 2.0 ** -21 * torch.randint(1, 3, (n, 1), generator=g)
+    cache, tables = cache_of(k, v, page)
+    _, v64 = R.values(cache.cpu().numpy())
+    v64 = v64.reshape(-1, 64)[:n]
+    seen = np.arange(n)[None] <= n - rows + np.arange(rows)[:, None]
+
+    def expect(q, scale, p, l):
+        out, lse = attend(q, cache, tables, n, scale, cut)
+        o = (p @ v64 / p.sum(1, keepdims=True))[:, None]
+        tol = U[q.dtype] * np.abs(o) + 2.0 ** -10 * np.abs(v64).max()
+        assert (np.abs(out - o) <= tol).all(), (scale, int(np.isnan(out).sum()))
+        assert (np.abs(lse[:, 0] - l) <= 2.0 ** -16 * np.abs(l)).all(), scale
+    # all scores 0 or next to it, with keys that the mask hides: the mean of the values that a row sees
+    p = seen.astype(float)
+    for dtype, size, scale in ((torch.bfloat16, 1e-38, 1e-10), (torch.bfloat16, 1e-39, 0.1), (torch.float16, 1.0, 1e-40), (torch.float16, 0.0, 1e30),
+                               (torch.bfloat16, 0.0, 1e30)):
+        expect(torch.full((rows, 1, 64), size).to(dtype).cuda(), scale, p, np.log(p.sum(1)))
+    # queries next to 2^128 where the keys are 0: 0 as well, for any scale below 2^13
+    q = torch.zeros(rows, 1, 64, dtype=torch.bfloat16, device="cuda")
+    q[:, :, :32] = 1.5 * 2.0 ** 127
+    for scale in (0.125, 1.9, 7.0, 5000.0, -5000.0):
+        expect(q, scale, p, np.log(p.sum(1)))
