@@ -199,6 +199,16 @@ __device__ __forceinline__ Scale scale_of(const AttnArgs& a, float top) {
     return s;
 }
 
+// The exponentials' arguments x * factor - reference are single operations, which is right while the reference, a rounded product, is within
+// half of the product itself.  From 2^22 on the products are rounded first, as the reference was: otherwise the largest key's exponential
+// would be 0 or infinite, whichever way the rounding went.
+constexpr float kFar = 0x1p22f;
+__device__ __forceinline__ bool is_far(float ref) { return __any(fabsf(ref) > kFar && fabsf(ref) < INFINITY); }
+__device__ __forceinline__ float rounded_product(float x, float factor) {
+#pragma clang fp contract(off)
+    return x * factor;
+}
+
 // One tile's bytes of one lane: [group of 16 tokens][words].
 template <int D>
 struct Raw {
@@ -294,6 +304,7 @@ __device__ __forceinline__ void segment(const AttnArgs& a, const Sequence& s, in
 
     f32x4 o[NT][CT];
     float m[NT], l[NT];
+    bool far = false;  // of any row of the wave
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         m[n] = -INFINITY, l[n] = 0;
@@ -378,10 +389,11 @@ __device__ __forceinline__ void segment(const AttnArgs& a, const Sequence& s, in
 #pragma unroll
             for (int j = 1; j < 8; ++j) top = fmaxf(top, x[n][j]);
             top *= factor[n];
-            if (__any(top > m[n] + kRaise)) {  // all four lanes of a row take the same reference
+            if (__any(top - m[n] > kRaise)) {  // all four lanes of a row take the same reference
                 top = fmaxf(top, __shfl_xor(top, 16));
                 top = fmaxf(top, __shfl_xor(top, 32));
                 const float to = fmaxf(m[n], top - kRoom);
+                far = far || is_far(to);
                 const float by = to == m[n] ? 1.f : __builtin_amdgcn_exp2f(m[n] - to);
                 m[n] = to;
                 l[n] *= by;
@@ -389,9 +401,15 @@ __device__ __forceinline__ void segment(const AttnArgs& a, const Sequence& s, in
                 for (int c = 0; c < CT; ++c) o[n][c] *= by;
             }
             const float ref = m[n] == -INFINITY ? 0.f : m[n];
+            float f = factor[n];
+            if (__builtin_expect(far, 0)) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[n][j] = rounded_product(x[n][j], f);
+                f = 1;
+            }
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float e = __builtin_amdgcn_exp2f(fmaf(x[n][j], factor[n], -ref));
+                const float e = __builtin_amdgcn_exp2f(fmaf(x[n][j], f, -ref));
                 l[n] += e;
                 p[n][j] = (_Float16)e;
             }
@@ -646,6 +664,7 @@ __device__ __forceinline__ void wide_segment(const AttnArgs& a, const Sequence& 
 #pragma unroll
         for (int v = 0; v < 16; ++v) o[c][v] = 0;
     float m = -INFINITY, l = 0;
+    bool far = false;  // as in `segment`
 
     // A step's products in their order: the next tile's scores (32 tokens s % 2, 16 channels s / 2) for s = 0, 1, .. and, from the first eight
     // exponentials on, this tile's outputs between them.
@@ -736,9 +755,10 @@ __device__ __forceinline__ void wide_segment(const AttnArgs& a, const Sequence& 
             top = largest();
         }
         top *= factor;
-        if (__any(top > m + kRaise)) {
+        if (__any(top - m > kRaise)) {
             top = fmaxf(top, __shfl_xor(top, 32));
             const float to = fmaxf(m, top - kRoom);
+            far = far || is_far(to);
             const float by = to == m ? 1.f : __builtin_amdgcn_exp2f(m - to);
             m = to;
             l *= by;
@@ -746,6 +766,14 @@ __device__ __forceinline__ void wide_segment(const AttnArgs& a, const Sequence& 
             for (int c = 0; c < CT; ++c) o[c] *= by;
         }
         const float ref = m == -INFINITY ? 0.f : m;
+        float f = factor;
+        if (__builtin_expect(far, 0)) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) x[i][v] = rounded_product(x[i][v], f);
+            f = 1;
+        }
         f16x8 p[4];
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -753,16 +781,16 @@ __device__ __forceinline__ void wide_segment(const AttnArgs& a, const Sequence& 
             for (int v = 0; v < 16; ++v) y[i][v] = 0;
         auto multiply = [&](int n) {
             const Product w = product(n);
-            const f16x8 f = __builtin_bit_cast(f16x8, op[n % kAhead]);
-            if (w.score) y[w.i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f, q[w.k], y[w.i], 0, 0, 0);
-            else o[w.k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f, p[w.i], o[w.k], 0, 0, 0);
+            const f16x8 with = __builtin_bit_cast(f16x8, op[n % kAhead]);
+            if (w.score) y[w.i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(with, q[w.k], y[w.i], 0, 0, 0);
+            else o[w.k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(with, p[w.i], o[w.k], 0, 0, 0);
             if (n + kAhead < kProducts) op[n % kAhead] = operand(n + kAhead, t);
         };
         int n = 0;
 #pragma unroll
         for (int j = 0; j < 32; ++j) {
             if (j * L / 8 * 8 == j * L && (j < 24 || j * L / 8 % 2 == 0)) multiply(n++);
-            const float e = __builtin_amdgcn_exp2f(fmaf(x[j / 16][j % 16], factor, -ref));
+            const float e = __builtin_amdgcn_exp2f(fmaf(x[j / 16][j % 16], f, -ref));
             l += e;
             p[j / 8][j % 8] = (_Float16)e;
         }

@@ -104,3 +104,48 @@ def test_scales_and_queries_whose_product_leaves_the_range_of_32_bits(form, cut)
     q[:, :, :32] = 1.5 * 2.0 ** 127
     for scale in (0.125, 1.9, 7.0, 5000.0, -5000.0):
         expect(q, scale, p, np.log(p.sum(1)))
+
+
+def one_largest(q, cache, tables, n, scale):
+    """Where each row's largest score is far above all others in 32 bits: the mean of the values of the keys that have it, and lse."""
+    k, v = (x.reshape(-1, q.shape[-1])[:n] for x in R.values(cache.cpu().numpy()))
+    rows = q.shape[0]
+    x = f64(q)[:, 0] @ k.T * scale
+    x[np.arange(n)[None] > n - rows + np.arange(rows)[:, None]] = -np.inf
+    top = x.max(1, keepdims=True)
+    p = (x == top).astype(float)
+    second = np.where(p > 0, -np.inf, x).max(1)
+    assert np.isfinite(top).all() and (top[:, 0] - second > 2.0 ** -8 * np.abs(top[:, 0])).all()
+    return (p @ v / p.sum(1, keepdims=True))[:, None], top + np.log(p.sum(1, keepdims=True))
+
+
+@pytest.mark.parametrize("cut", [True, False], ids=["cut", "uncut"])
+@pytest.mark.parametrize("form", FORMS)
+def test_scores_of_any_size(form, cut):
+    """Scores from 1e5 to 1e37, of both signs, far beyond what neighbouring numbers in 32 bits can tell apart by less than 1."""
+    n, rows, page = FORMS[form]
+    g = torch.Generator().manual_seed(rows)
+    for dtype, size, scale in ((torch.float16, 3.0, 1e4), (torch.float16, 2e3, 1.7), (torch.float16, 3e4, 1.3), (torch.float16, 3e4, -0.7),
+                               (torch.bfloat16, 1e8, 0.125), (torch.bfloat16, 3e30, 1.9), (torch.bfloat16, 3e30, -1.1)):
+        base = torch.randint(1, 7, (64,), generator=g) * 2.0 ** 12
+        k = base[None] * torch.where(torch.arange(n) % 7 == 3, 1.0, 0.5)[:, None]
+        k[-rows:] = 0                                              # every row sees the same of the other keys
+        k[-rows:, 0] = base[0] * 0.75                              # one channel: the largest where the scale turns all scores
+        v = torch.randn(n, 64, generator=g)
+        cache, tables = cache_of(k, v, page)
+        q = ((torch.rand(rows, 1, 64, generator=g) * 0.5 + 0.5) * size).to(dtype).cuda()
+        out, lse = attend(q, cache, tables, n, scale, cut)
+        o, l = one_largest(q, cache, tables, n, scale)
+        tol = U[dtype] * np.abs(o) + 2.0 ** -10 * np.abs(f64(v)).max()
+        assert (np.abs(out - o) <= tol).all(), (dtype, size, scale, float(np.nanmax(np.abs(out - o) / tol)), int(np.isnan(out).sum()))
+        assert (np.abs(lse - l) <= 2.0 ** -16 * np.abs(l)).all(), (dtype, size, scale)
+    # queries next to 2^127, where the keys are small
+    k[-rows:] = 0
+    cache, tables = cache_of(k * 2.0 ** -34, v, page)
+    q = ((torch.rand(rows, 1, 64, generator=g) * 0.5 + 0.5) * 2.0 ** 127).bfloat16().cuda()
+    for scale in (0.125, 7.0, 500.0):
+        out, lse = attend(q, cache, tables, n, scale, cut)
+        o, l = one_largest(q, cache, tables, n, scale)
+        tol = U[q.dtype] * np.abs(o) + 2.0 ** -10 * np.abs(f64(v)).max()
+        assert (np.abs(out - o) <= tol).all(), (scale, int(np.isnan(out).sum()))
+        assert (np.abs(lse - l) <= 2.0 ** -16 * np.abs(l)).all(), scale
