@@ -181,6 +181,18 @@ def takes_memory(stream: int, device) -> bool:
     return stream == torch.cuda.current_stream(device).cuda_stream and stream != 2     # 2: hipStreamPerThread, a queue of every thread
 
 
+def scratch(bytes_: int, stream: int, device):
+    """Scratch memory of one call on `stream` from torch's allocator, or None where the call may not take any.  In a graph that torch records it
+    comes from that graph's own pool; a recording begun elsewhere would keep the address of memory that torch hands on at once, and gets none."""
+    import torch
+    if not takes_memory(stream, device):
+        return None
+    with torch.cuda.device(device):
+        capturing = lib().gemm_lrelu_capturing(ctypes.c_void_p(stream))
+    memory = torch.empty(bytes_, dtype=torch.uint8, device=device)
+    return memory if not capturing or native().memory_of_a_pool(memory.data_ptr()) is True else None
+
+
 def attn_fwd(q, k, v, out, lse, causal: bool, scale: float, stream=None) -> None:
     """out, lse <- fused attention forward of device tensors q, k, v ([B,H,N,d]).
     Asynchronous on `stream` (an integer hipStream_t; default: torch's current stream)."""

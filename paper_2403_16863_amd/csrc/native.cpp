@@ -39,12 +39,21 @@ decltype(&qk_norm_rope) g_rope = nullptr;
 decltype(&qk_norm_rope_bwd) g_rope_bwd = nullptr;
 decltype(&qk_norm_rope_bwd_workspace) g_rope_bwd_workspace = nullptr;
 
+// Whether torch's allocator has an address in a pool of its own: one that it opened for a graph that it records (or its user for tensors).  It looks
+// through all segments, which a recording can wait for.
+bool in_private_pool(const void* p) {
+    for (const auto& s : c10::hip::HIPCachingAllocator::snapshot().segments)
+        if ((size_t)p - s.address < s.total_size) return s.owner_private_pool_id.first || s.owner_private_pool_id.second;
+    return false;
+}
+
 // Scratch memory of one call, from torch's caching allocator: it belongs to the stream the call runs on, so it
 // may go back as soon as the kernels are enqueued (the next owner on that stream comes after them).  That holds
 // where a handle is one queue and outlives its work: torch's current stream, but not a handle that only the
 // caller knows, nor the per-thread stream, one handle for a queue of every thread.  No memory either
-// on a device that is not the current one, or when there is none left, or, unless `captured`, while the stream is captured; the
-// call then does without.  In a graph that torch records the memory comes from that graph's own pool and stays its.
+// on a device that is not the current one, or when there is none left, or while the stream is captured, unless `captured` and torch itself records: in its
+// graph the memory comes from that graph's own pool and stays its, but a recording begun elsewhere would keep the address of memory that torch hands on at once.
+// The call then does without.
 class Workspace {
   public:
     Workspace(void* stream, int device, bool captured = false) : stream_(stream), device_(device), captured_(captured) {}
@@ -53,13 +62,17 @@ class Workspace {
     void* take(long long bytes) {
         try {
             if (stream_ != (void*)c10::hip::getCurrentHIPStream(device_).stream() || stream_ == (void*)hipStreamPerThread ||
-                c10::hip::current_device() != device_ || (!captured_ && g_capturing(stream_)))
+                c10::hip::current_device() != device_)
                 return nullptr;
+            const bool capturing = g_capturing(stream_);
+            if (capturing && !captured_) return nullptr;
             // A recording in another thread (in the default mode) forbids this thread the allocator's calls to the
             // device, and one such call would end it; they have nothing to do with it.
             const c10::hip::HIPStreamCaptureModeGuard beside(hipStreamCaptureModeRelaxed);
             p_ = c10::hip::HIPCachingAllocator::raw_alloc_with_stream((size_t)bytes, (hipStream_t)stream_);
+            if (capturing && !in_private_pool(p_)) return nullptr;
         } catch (const std::exception&) {
+            return nullptr;
         }
         return p_;
     }
@@ -413,6 +426,12 @@ PyObject* norm_rope_bwd(PyObject* const* args, Py_ssize_t nargs) {
     return PyLong_FromLong(rc);
 }
 
+// memory_of_a_pool(address): whether torch's allocator has it in a pool other than the common one
+PyObject* memory_of_a_pool(PyObject* const* args, Py_ssize_t nargs) {
+    if (nargs != 1) return not_plain();
+    return PyBool_FromLong(in_private_pool(PyLong_AsVoidPtr(args[0])));
+}
+
 // bind_cached(addresses of kv4_append, kv4_read, kv4_attn, kv4_attn_workspace, qk_norm_rope, qk_norm_rope_bwd and qk_norm_rope_bwd_workspace)
 PyObject* bind_cached(PyObject*, PyObject* args) {
     unsigned long long f[7];
@@ -440,6 +459,7 @@ PyMethodDef methods[] = {{"attn_fwd", (PyCFunction)(void (*)(void))guarded<attn_
                          {"kv4_attn", (PyCFunction)(void (*)(void))guarded<cached_attn>, METH_FASTCALL, "0, a library error, or NOT_PLAIN"},
                          {"qk_norm_rope", (PyCFunction)(void (*)(void))guarded<norm_rope>, METH_FASTCALL, "0, a library error, or NOT_PLAIN"},
                          {"qk_norm_rope_bwd", (PyCFunction)(void (*)(void))guarded<norm_rope_bwd>, METH_FASTCALL, "0, a library error, or NOT_PLAIN"},
+                         {"memory_of_a_pool", (PyCFunction)(void (*)(void))guarded<memory_of_a_pool>, METH_FASTCALL, "whether an address is a private pool's"},
                          {"bind_cached", bind_cached, METH_VARARGS, "addresses of the library's entry points"},
                          {"bind", bind, METH_VARARGS, "addresses of the library's entry points"},
                          {nullptr, nullptr, 0, nullptr}};

@@ -196,8 +196,8 @@ def kv4_attn(q, cache, tables, lens, out, lse, causal: bool, scale: float, cu_q=
 
     Few long sequences are cut into runs of keys for which the call needs scratch memory: `workspace` (uint8,
     kv4_attn_workspace bytes), or, on torch's current stream, memory that it takes from torch's allocator itself (the graph's own
-    pool while torch records one; recordings begun elsewhere need the argument).  On another stream without a workspace the keys are
-    not cut, which is slower."""
+    pool while torch records one).  On another stream, or in a recording begun elsewhere, the keys are not cut without a workspace, which
+    is slower."""
     rc = _plain_attn(q, cache, tables, lens, out, lse, causal, scale, cu_q, max_q, workspace, stream)
     if not rc:
         return
@@ -235,8 +235,8 @@ def kv4_attn(q, cache, tables, lens, out, lse, causal: bool, scale: float, cu_q=
     if workspace is not None:
         if not workspace.is_contiguous() or workspace.numel() * workspace.element_size() < need:
             raise ValueError(f"workspace must be contiguous with {need} bytes")
-    elif need and binding.takes_memory(st, cache.device):
-        workspace = torch.empty(need, dtype=torch.uint8, device=cache.device)
+    elif need:
+        workspace = binding.scratch(need, st, cache.device)
     with torch.cuda.device(cache.device):
         rc = lib().kv4_attn(q.data_ptr(), cache.data_ptr(), tables.data_ptr(), lens.data_ptr(), _ptr(cu_q), out.data_ptr(), lse.data_ptr(),
                             T, B, H, heads, d, pages, page_size, width, int(max_q), int(bool(causal)), float(scale), dt, _ptr(workspace),

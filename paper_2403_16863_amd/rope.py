@@ -158,8 +158,8 @@ def qk_norm_rope_bwd(dq_out, dk_out, q, k, dq, dk, cos, sin, positions, q_weight
     """dq, dk, dq_weight, dk_weight <- gradients of qk_norm_rope, from those of its outputs and its inputs q, k (not needed, and
     None will do, for a tensor without a weight).  dq_weight, dk_weight: float32 [d], written.  With a weight
     the call needs scratch memory: `workspace` (uint8, qk_norm_rope_bwd_workspace bytes), or, on torch's current stream,
-    memory that it takes from torch's allocator itself (the graph's own pool while torch records one; recordings begun
-    elsewhere need the argument)."""
+    memory that it takes from torch's allocator itself (the graph's own pool while torch records one).  On another stream, and in
+    a recording begun elsewhere, the call is refused without the argument."""
     rc = _plain_norm_rope_bwd(dq_out, dk_out, q, k, dq, dk, cos, sin, positions, q_weight, k_weight, dq_weight, dk_weight, eps, interleaved,
                               workspace, stream)
     if not rc:
@@ -192,9 +192,9 @@ def qk_norm_rope_bwd(dq_out, dk_out, q, k, dq, dk, cos, sin, positions, q_weight
     if q_weight is not None or k_weight is not None:
         need = qk_norm_rope_bwd_workspace(B, N, H, Hkv, d)
         if workspace is None:
-            if not binding.takes_memory(st, like.device):
-                raise ValueError("a stream that is not torch's current one needs a workspace")
-            workspace = torch.empty(need, dtype=torch.uint8, device=like.device)
+            workspace = binding.scratch(need, st, like.device)
+            if workspace is None:
+                raise ValueError("a stream that is not torch's current one, or a recording that torch did not begin, needs a workspace")
         elif not workspace.is_contiguous() or workspace.numel() * workspace.element_size() < need:
             raise ValueError(f"workspace must be contiguous with {need} bytes")
     with torch.cuda.device(like.device):
