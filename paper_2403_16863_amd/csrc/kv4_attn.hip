@@ -1065,6 +1065,8 @@ int check_sizes(long long T, int B, int H, int heads, int d, int page_size, int 
     if (d != 64 && d != 128) return KV4_EUNSUPPORTED;
     const long long cap = (long long)width * page_size, rows = (long long)(H / heads) * max_q;
     if (cap > INT_MAX - 65535 || rows > 1 << 30 || B > 65535 || T * H > INT_MAX) return KV4_EUNSUPPORTED;
+    // The refusal below, for the largest row blocks and in numbers that do not wrap around.
+    if ((double)B * (double)((rows + 255) / 256) * heads >= 1 << 23) return KV4_EUNSUPPORTED;
     const Choice c = choose(T, B, H, heads, d, cap, max_q);
     // Positions and rows of pieces are counted in 32 bits, and so are keys up to the end of the last tile.
     return c.blocks >= 1 << 23 || (c.bytes && (double)(c.blocks + c.target) * (double)(cap / kTile + 32) > INT_MAX) ? KV4_EUNSUPPORTED : KV4_OK;

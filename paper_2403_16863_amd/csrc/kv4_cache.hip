@@ -200,7 +200,7 @@ int check_cache(const void* cache, int heads, int d, int pages, int page_size) {
 }
 
 // Threads of a launch are counted in 32 bits.
-bool too_many(long long T, int heads, int d) { return (T + 15) / 16 * 16 * heads * (d / 16) > 0xffffff00LL; }
+bool too_many(long long T, int heads, int d) { return (double)((T + 15) / 16 * 16) * heads * (d / 16) > 0xffffff00LL; }
 
 int launch(const void* fn, unsigned grid, void* args, void* stream) {
     void* list[] = {args};

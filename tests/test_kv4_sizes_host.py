@@ -1,0 +1,25 @@
+"""Sizes of the cache's calls whose products pass 64 bits: refused, without a GPU."""
+import ctypes
+
+from paper_2403_16863_amd import kv4
+
+
+def p(x):
+    return ctypes.c_void_p(x)
+
+
+def test_segments_that_wrap_around_are_refused():
+    """2^15 sequences of 2^30 rows in each of 2^26 heads are 2^64 row blocks and more."""
+    L, heads = kv4.lib(), 1 << 26
+    for width in (2, 1000):
+        assert L.kv4_attn_workspace(1, 1 << 15, heads, heads, 64, 16, width, 1 << 30) == kv4.KV4_EUNSUPPORTED
+        assert L.kv4_attn(p(0x100000), p(1 << 44), p(0x300000), p(0x400000), p(0x500000), p(1 << 45), p(0x700000), 1, 1 << 15, heads, heads, 64, 1, 16,
+                          width, 1 << 30, 1, 0.1, 0, None, 0, None) == kv4.KV4_EUNSUPPORTED
+    assert L.kv4_attn_workspace(1, 65535, (1 << 31) - 1, (1 << 31) - 1, 64, 16, 2, 1 << 30) == kv4.KV4_EUNSUPPORTED
+
+
+def test_threads_that_wrap_around_are_refused():
+    L, T, heads = kv4.lib(), (1 << 31) - 1, 1 << 30
+    assert L.kv4_append(p(0x10000), 64, 64, p(0x20000), 64, 64, p(0x30000), p(0x40000), None, None, None, 0, 0, T, heads, 128, 3, 16, 0,
+                        None) == kv4.KV4_EUNSUPPORTED
+    assert L.kv4_read(p(0x30000), p(0x40000), p(0x10000), None, T, heads, 128, 3, 16, 0, None) == kv4.KV4_EUNSUPPORTED
