@@ -81,6 +81,12 @@ def _ints(name, t, shape):
         raise ValueError(f"{name} must be contiguous int32 {list(shape)}")
 
 
+def _fit(what, *sizes):
+    """The library counts in 32 bits, and ctypes would cut a larger number to them."""
+    if max(sizes) > 2 ** 31 - 1 or min(sizes) < -2 ** 31:
+        raise Kv4Error(KV4_EUNSUPPORTED, what)
+
+
 def _dtype_code(t) -> int:
     import torch
     if t.dtype == torch.float16:
@@ -141,6 +147,7 @@ def kv4_append(k, v, cache, slots, cos=None, sin=None, positions=None, interleav
                 raise ValueError(f"{name} must be contiguous float32 [rows,d/2]")
         _ints("positions", positions, (T,))
         rows = cos.shape[0]
+    _fit("kv4_append", T, rows, pages)
     ks, vs = ([t.stride(0) if T > 1 else 0, t.stride(1) if heads > 1 else 0] for t in (k, v))
     if T == 0:
         return
@@ -172,6 +179,7 @@ def kv4_read(cache, slots, k=None, v=None, stream=None) -> None:
             raise ValueError("k and v must share one dtype")
     T, dt = like.shape[0], _dtype_code(like)
     _ints("slots", slots, (T,))
+    _fit("kv4_read", T, pages)
     if T == 0:
         return
     with torch.cuda.device(cache.device):
@@ -183,7 +191,9 @@ def kv4_read(cache, slots, k=None, v=None, stream=None) -> None:
 
 def kv4_attn_workspace(T: int, B: int, H: int, heads: int, d: int, page_size: int, width: int, max_q: int) -> int:
     """Bytes of scratch memory that kv4_attn has a use for (0: none)."""
-    n = lib().kv4_attn_workspace(int(T), int(B), int(H), int(heads), int(d), int(page_size), int(width), int(max_q))
+    sizes = [int(x) for x in (T, B, H, heads, d, page_size, width, max_q)]
+    _fit("kv4_attn_workspace", *sizes)
+    n = lib().kv4_attn_workspace(*sizes)
     if n < 0:
         raise Kv4Error(n, "kv4_attn_workspace")
     return n
@@ -230,6 +240,7 @@ def kv4_attn(q, cache, tables, lens, out, lse, causal: bool, scale: float, cu_q=
         return
     if cu_q is None:
         max_q = T // B
+    _fit("kv4_attn", T, B, width, int(max_q), pages)
     st = _stream(stream, cache.device)
     need = kv4_attn_workspace(T, B, H, heads, d, page_size, width, max_q)
     if workspace is not None:

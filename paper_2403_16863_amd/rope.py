@@ -52,6 +52,12 @@ class RopeError(RuntimeError):
         self.code = code
 
 
+def _fit(what, *sizes):
+    """The library counts in 32 bits, and ctypes would cut a larger number to them."""
+    if max(sizes) > 2 ** 31 - 1 or min(sizes) < -2 ** 31:
+        raise RopeError(QK_EUNSUPPORTED, what)
+
+
 def _check_heads(name, t, like, heads=None):
     if t is None:
         return
@@ -137,6 +143,7 @@ def qk_norm_rope(q, k, q_out, k_out, cos, sin, positions, q_weight=None, k_weigh
                       (("q", q), ("k", k), ("q_out", q_out), ("k_out", k_out), ("cos", cos), ("sin", sin), ("positions", positions),
                        ("q_weight", q_weight), ("k_weight", k_weight)))
     B, N, _, d = like.shape
+    _fit("qk_norm_rope", B, N, H, Hkv, cos.shape[0])
     hs = [_heads(t) for t in (q, k, q_out, k_out)]
     with torch.cuda.device(like.device):
         rc = lib().qk_norm_rope(*hs, _ptr(q_weight), _ptr(k_weight), f32, cos.data_ptr(), sin.data_ptr(), positions.data_ptr(), cos.shape[0],
@@ -147,7 +154,9 @@ def qk_norm_rope(q, k, q_out, k_out, cos, sin, positions, q_weight=None, k_weigh
 
 def qk_norm_rope_bwd_workspace(B: int, N: int, H: int, Hkv: int, d: int) -> int:
     """Bytes of scratch memory that qk_norm_rope_bwd needs where there is a weight."""
-    n = lib().qk_norm_rope_bwd_workspace(int(B), int(N), int(H), int(Hkv), int(d))
+    sizes = [int(x) for x in (B, N, H, Hkv, d)]
+    _fit("qk_norm_rope_bwd_workspace", *sizes)
+    n = lib().qk_norm_rope_bwd_workspace(*sizes)
     if n < 0:
         raise RopeError(n, "qk_norm_rope_bwd_workspace")
     return n
@@ -184,6 +193,7 @@ def qk_norm_rope_bwd(dq_out, dk_out, q, k, dq, dk, cos, sin, positions, q_weight
                        ("positions", positions), ("q_weight", q_weight), ("k_weight", k_weight), ("dq_weight", dq_weight),
                        ("dk_weight", dk_weight), ("workspace", workspace)))
     B, N, _, d = like.shape
+    _fit("qk_norm_rope_bwd", B, N, H, Hkv, cos.shape[0])
     for w in (dq_weight, dk_weight):
         if w is not None and (w.dtype != torch.float32 or tuple(w.shape) != (d,) or not w.is_contiguous()):
             raise ValueError("gradients of weights must be contiguous float32 [d]")

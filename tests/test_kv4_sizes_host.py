@@ -23,3 +23,30 @@ def test_threads_that_wrap_around_are_refused():
     assert L.kv4_append(p(0x10000), 64, 64, p(0x20000), 64, 64, p(0x30000), p(0x40000), None, None, None, 0, 0, T, heads, 128, 3, 16, 0,
                         None) == kv4.KV4_EUNSUPPORTED
     assert L.kv4_read(p(0x30000), p(0x40000), p(0x10000), None, T, heads, 128, 3, 16, 0, None) == kv4.KV4_EUNSUPPORTED
+
+
+def test_python_sizes_beyond_an_int_are_refused():
+    """Not cut to 32 bits: 2^32 + 1 queries of a sequence are not one."""
+    import pytest
+    import torch
+    from torch._subclasses.fake_tensor import FakeTensorMode
+
+    from paper_2403_16863_amd import rope
+    for bad in ((1, 1, 4, 2, 64, 16, 500, (1 << 32) + 1), (1, 1, 4, 2, 64, 16, (1 << 32) + 500, 1), (1 << 40, 1, 4, 2, 64, 16, 500, 1)):
+        with pytest.raises(kv4.Kv4Error) as e:
+            kv4.kv4_attn_workspace(*bad)
+        assert e.value.code == kv4.KV4_EUNSUPPORTED
+    with pytest.raises(rope.RopeError) as e:
+        rope.qk_norm_rope_bwd_workspace(1, (1 << 32) + 1, 4, 2, 64)
+    assert e.value.code == rope.QK_EUNSUPPORTED
+    with FakeTensorMode():
+        z = lambda *s, dtype=torch.float16: torch.empty(*s, dtype=dtype, device="cuda")  # noqa: E731
+        i32, many = torch.int32, (1 << 32) + 4
+        cache, q, lens, cu = z(3, 2, 16, 68, dtype=torch.uint8), z(4, 4, 64), z(2, dtype=i32), z(3, dtype=i32)
+        k = z(1, 2, 64).expand(many, 2, 64)
+        for call in (lambda: kv4.kv4_attn(q, cache, z(2, 5, dtype=i32), lens, q, z(4, 4, dtype=torch.float32), True, 1.0, cu, (1 << 32) + 1),
+                     lambda: kv4.kv4_append(k, k, cache, z(many, dtype=i32)),
+                     lambda: kv4.kv4_read(cache, z(many, dtype=i32), z(many, 2, 64))):
+            with pytest.raises(kv4.Kv4Error) as e:
+                call()
+            assert e.value.code == kv4.KV4_EUNSUPPORTED
