@@ -65,7 +65,7 @@ int kv4_read(const void* cache, const int* slots, void* k, void* v, int T, int h
  *     x_j = scale * q . k_j,   lse = ln sum_j exp(x_j),   out = sum_j exp(x_j - lse) v_j
  * A row that sees no key gets out = 0 and lse = -infinity.
  *
- *  q, out : device, [T, H, d] contiguous, 16-byte aligned; lse: device, fp32 [T, H].  out must not overlap q, lse or the cache.  Rows of q before cu_q[0]
+ *  q, out : device, [T, H, d] contiguous, 16-byte aligned; lse: device, fp32 [T, H].  out, lse and the workspace overlap nothing.  Rows of q before cu_q[0]
  *           and from cu_q[B] on belong to nobody: their out and lse stay as they are.
  *  tables : device, int32 [B, width].  Only the entries of pages that hold keys below lens[b] are read; keys of an entry outside
  *           0 .. pages-1 are not seen.  lens: device, int32 [B]; counts above width * page_size are taken as that, negative ones as 0.

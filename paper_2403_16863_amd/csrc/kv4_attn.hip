@@ -1122,9 +1122,14 @@ int kv4_attn(const void* q, const void* cache, const int* tables, const int* len
     if ((long long)pages * page_size > INT_MAX || (long long)pages * heads * (page_size / 16) > UINT_MAX) return KV4_EUNSUPPORTED;
     const long long bytes = (long long)T * H * d * 2;
     const long long held = (long long)pages * heads * page_size * (d + d / 16);
-    if (overlap(q, bytes, out, bytes) || overlap(lse, (long long)T * H * 4, out, bytes) || overlap(cache, held, out, bytes)) return KV4_EINVAL;
+    const long long lse_bytes = (long long)T * H * 4;
+    if (overlap(q, bytes, out, bytes) || overlap(lse, lse_bytes, out, bytes) || overlap(cache, held, out, bytes)) return KV4_EINVAL;
+    if (overlap(q, bytes, lse, lse_bytes) || overlap(cache, held, lse, lse_bytes)) return KV4_EINVAL;
     const Choice c = choose(T, B, H, heads, d, (long long)width * page_size, max_q);
     const bool cut = c.bytes && workspace && workspace_bytes >= c.bytes;
+    if (cut && (overlap(q, bytes, workspace, c.bytes) || overlap(out, bytes, workspace, c.bytes) || overlap(lse, lse_bytes, workspace, c.bytes) ||
+                overlap(cache, held, workspace, c.bytes)))
+        return KV4_EINVAL;
     AttnArgs a = {(const uint16_t*)q, (const uint8_t*)cache, tables, lens, cu_q, (uint16_t*)out, lse, cut ? (int2*)workspace : nullptr,
                   cut ? (float*)((char*)workspace + c.bytes - c.slots * c.rows * (d + 2) * 4) : nullptr, T, B, H,
                   heads, H / heads, pages, __builtin_ctz(page_size), width, max_q, causal, scale * 1.4426950408889634f, c.target};

@@ -50,3 +50,18 @@ def test_python_sizes_beyond_an_int_are_refused():
             with pytest.raises(kv4.Kv4Error) as e:
                 call()
             assert e.value.code == kv4.KV4_EUNSUPPORTED
+
+
+def test_attention_refuses_outputs_and_scratch_memory_over_its_inputs():
+    L = kv4.lib()
+    q, cache, out, lse, ws, cap = 0x1000000, 0x2000000, 0x3000000, 0x4000000, 0x5000000, 64
+    need = L.kv4_attn_workspace(4, 2, 4, 2, 64, 16, 500, 3)
+    assert need > 0
+
+    def call(q=q, cache=cache, out=out, lse=lse, ws=ws, room=need):
+        return L.kv4_attn(p(q), p(cache), p(0x6000000), p(0x7000000), p(0x8000000), p(out), p(lse), 4, 2, 4, 2, cap, 3, 16, 500, 3, 1, 0.1, 0, p(ws),
+                          room, None)
+    # T * H * d * 2 = 2048 bytes of q and out, 64 of lse, 3 * 2 * 16 * 68 = 6528 of the cache
+    for bad in (dict(lse=q), dict(lse=q + 2044), dict(lse=cache + 6524), dict(lse=cache - 60), dict(ws=q), dict(ws=q - need + 16), dict(ws=out + 2032),
+                dict(ws=lse + 48), dict(ws=cache + 6512), dict(ws=cache - need + 16)):
+        assert call(**bad) == kv4.KV4_EINVAL, bad
