@@ -17,8 +17,9 @@
  * bfloat16.  Larger values become 49152.  32 channels that hold an infinity or a NaN become NaN.
  *
  * General rules (those of attn.h): device pointers are the caller's, nothing is allocated, cleared or waited for, calls are asynchronous
- * on `stream` and may be recorded into a graph; KV4_OK or a negative error comes back, on an error nothing has been
- * enqueued; no C++ exception crosses this boundary.  dtype: KV4_F16 or KV4_BF16 for all 16-bit elements of a call.
+ * on `stream` and may be recorded into a graph; KV4_OK or a negative error comes back.  On KV4_EINVAL and KV4_EUNSUPPORTED nothing has been
+ * enqueued.  After KV4_ELAUNCH the first of kv4_attn's two kernels may have been: its memory is in use until the
+ * stream has run, and what it writes is undefined.  No C++ exception crosses this boundary.  dtype: KV4_F16 or KV4_BF16 for all 16-bit elements of a call.
  * Indices (slots, positions, tables, lengths) are read on the device and may change between replays of a graph.
  */
 #ifndef PAPER_2403_16863_AMD_KV4_H

@@ -9,8 +9,9 @@
  *     dw = sum over tokens and heads of g r x,      dx = r (h - r x mean_i(h_i r x_i)),      without a weight dx = g.
  *
  * General rules (those of attn.h): device pointers are the caller's, nothing is allocated, cleared or waited for, calls are asynchronous
- * on `stream` and may be recorded into a graph; QK_OK or a negative error comes back, on an error nothing has been
- * enqueued; no C++ exception crosses this boundary.
+ * on `stream` and may be recorded into a graph; QK_OK or a negative error comes back.  On QK_EINVAL and QK_EUNSUPPORTED nothing has been
+ * enqueued.  After QK_ELAUNCH the first of qk_norm_rope_bwd's two kernels may have been: its memory is in use until the
+ * stream has run, and what it writes is undefined.  No C++ exception crosses this boundary.
  */
 #ifndef PAPER_2403_16863_AMD_QK_ROPE_H
 #define PAPER_2403_16863_AMD_QK_ROPE_H
