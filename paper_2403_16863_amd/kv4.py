@@ -202,7 +202,7 @@ def kv4_attn_workspace(T: int, B: int, H: int, heads: int, d: int, page_size: in
 def kv4_attn(q, cache, tables, lens, out, lse, causal: bool, scale: float, cu_q=None, max_q=None, workspace=None, stream=None) -> None:
     """out [T,H,d], lse [T,H] <- attention of q [T,H,d] over the cache.  Sequence b has lens[b] keys in the pages tables[b] and, with cu_q
     (int32 [B+1]), the queries cu_q[b] .. cu_q[b+1] - 1, at most max_q of them; without it T / B queries.  causal: the
-    last query of a sequence sees its last key.  All contiguous; tables int32 [B,width], lens int32 [B], lse float32.
+    last query of a sequence sees its last key.  Nothing is recorded for autograd.  All contiguous; tables int32 [B,width], lens int32 [B], lse float32.
 
     Few long sequences are cut into runs of keys for which the call needs scratch memory: `workspace` (uint8,
     kv4_attn_workspace bytes), or, on torch's current stream, memory that it takes from torch's allocator itself (the graph's own

@@ -124,8 +124,8 @@ def qk_norm_rope(q, k, q_out, k_out, cos, sin, positions, q_weight=None, k_weigh
                  stream=None) -> None:
     """q_out, k_out <- norm (where there is a weight) and rotation of q [B,N,H,d] and k [B,N,Hkv,d].  All four may have any
     strides that divide by 8 with contiguous channels: slices of a joint projection, or the transposed view of attn_fwd's [B,H,N,d];
-    q or k may be None with its output.  cos, sin: float32 [rows,d/2]; positions: int32 [B,N].  Asynchronous on `stream` (an
-    integer hipStream_t; default: torch's current stream)."""
+    q or k may be None with its output.  cos, sin: float32 [rows,d/2]; positions: int32 [B,N].  Nothing is recorded for
+    autograd: qk_norm_rope_bwd gives the gradients.  Asynchronous on `stream` (an integer hipStream_t; default: torch's current stream)."""
     rc = _plain_norm_rope(q, k, q_out, k_out, cos, sin, positions, q_weight, k_weight, eps, interleaved, stream)
     if not rc:
         return
