@@ -56,7 +56,8 @@ int kv4_append(const void* k, long long k_token_stride, long long k_head_stride,
                int rows, int interleaved, int T, int heads, int d, int pages, int page_size, int dtype, void* stream);
 
 /* The values that the cache holds in the given slots: k, v (device, [T, heads, d] contiguous, 16-byte aligned) <- slot slots[t]
- * of every head, exact in `dtype`; zeros for a slot outside the cache.  Either of k and v may be null. */
+ * of every head, exact in `dtype`; zeros for a slot outside the cache.  Either of k and v may be null; they overlap neither each other
+ * nor the cache. */
 int kv4_read(const void* cache, const int* slots, void* k, void* v, int T, int heads, int d, int pages, int page_size, int dtype,
              void* stream);
 

@@ -1100,10 +1100,6 @@ int launch_attn(const Choice& c, AttnArgs& a, void* stream) {
     return KV4_OK;
 }
 
-bool overlap(const void* a, long long an, const void* b, long long bn) {
-    return (uintptr_t)a < (uintptr_t)b + bn && (uintptr_t)b < (uintptr_t)a + an;
-}
-
 }  // namespace kv4
 
 extern "C" {

@@ -242,6 +242,8 @@ int kv4_read(const void* cache, const int* slots, void* k, void* v, int T, int h
     if (const int rc = check_cache(cache, heads, d, pages, page_size)) return rc;
     if (too_many(T, heads, d)) return KV4_EUNSUPPORTED;
     if (T == 0) return KV4_OK;
+    const long long bytes = (long long)T * heads * d * 2, held = (long long)pages * page_size * heads * (d + d / 16);
+    if ((k && v && overlap(k, bytes, v, bytes)) || (k && overlap(k, bytes, cache, held)) || (v && overlap(v, bytes, cache, held))) return KV4_EINVAL;
     ReadArgs a = {(const uint8_t*)cache, slots, (uint16_t*)k, (uint16_t*)v, T, heads, pages * page_size, __builtin_ctz(page_size)};
     const unsigned grid = (unsigned)((((long long)T + 15) / 16 * 16 * heads * (d / 16) + 255) / 256);
     const void* fn = d == 128 ? (dtype ? (const void*)read_kernel<128, true> : (const void*)read_kernel<128, false>)

@@ -8,6 +8,11 @@ namespace kv4 {
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
+// Whether an bytes at a and bn at b meet.
+inline bool overlap(const void* a, long long an, const void* b, long long bn) {
+    return (uintptr_t)a < (uintptr_t)b + bn && (uintptr_t)b < (uintptr_t)a + an;
+}
+
 // 16 tokens of one head.
 template <int D>
 struct Group {

@@ -65,3 +65,13 @@ def test_attention_refuses_outputs_and_scratch_memory_over_its_inputs():
     for bad in (dict(lse=q), dict(lse=q + 2044), dict(lse=cache + 6524), dict(lse=cache - 60), dict(ws=q), dict(ws=q - need + 16), dict(ws=out + 2032),
                 dict(ws=lse + 48), dict(ws=cache + 6512), dict(ws=cache - need + 16)):
         assert call(**bad) == kv4.KV4_EINVAL, bad
+
+
+def test_reads_refuse_outputs_over_each_other_or_the_cache():
+    L = kv4.lib()
+    # 4 * 2 * 64 * 2 = 1024 bytes of k and v, 3 * 2 * 16 * 68 = 6528 of the cache
+
+    def call(k=0x10000, v=0x20000, cache=0x30000):
+        return L.kv4_read(p(cache), p(0x40000), p(k), p(v), 4, 2, 64, 3, 16, 0, None)
+    for bad in (dict(k=0x20000), dict(k=0x20000 + 1008), dict(v=0x10000 - 1008), dict(k=0x30000), dict(v=0x30000 + 6512), dict(k=0x30000 - 1008)):
+        assert call(**bad) == kv4.KV4_EINVAL, bad
