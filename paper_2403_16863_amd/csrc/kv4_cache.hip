@@ -7,6 +7,8 @@
 #include <limits.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "../../include/kv4.h"
 #include "kv4_format.h"
 
@@ -242,7 +244,8 @@ int kv4_read(const void* cache, const int* slots, void* k, void* v, int T, int h
     if (const int rc = check_cache(cache, heads, d, pages, page_size)) return rc;
     if (too_many(T, heads, d)) return KV4_EUNSUPPORTED;
     if (T == 0) return KV4_OK;
-    const long long bytes = (long long)T * heads * d * 2, held = (long long)pages * page_size * heads * (d + d / 16);
+    const long long bytes = (long long)T * heads * d * 2;
+    const long long held = (long long)std::min((double)pages * page_size * heads * (d + d / 16), 0x1p60);  // no cache is that large
     if ((k && v && overlap(k, bytes, v, bytes)) || (k && overlap(k, bytes, cache, held)) || (v && overlap(v, bytes, cache, held))) return KV4_EINVAL;
     ReadArgs a = {(const uint8_t*)cache, slots, (uint16_t*)k, (uint16_t*)v, T, heads, pages * page_size, __builtin_ctz(page_size)};
     const unsigned grid = (unsigned)((((long long)T + 15) / 16 * 16 * heads * (d / 16) + 255) / 256);
