@@ -24,7 +24,7 @@ enum { QK_F16 = 0, QK_BF16 = 1 };
 
 enum {
     QK_OK = 0,
-    QK_EINVAL = -1,       /* null or misaligned pointer, bad size, stride, dtype or eps, no workspace */
+    QK_EINVAL = -1,       /* null or misaligned pointer, an output over another tensor, bad size, stride, dtype or eps, no workspace */
     QK_EUNSUPPORTED = -2, /* head_dim other than 64 or 128; B * N * heads beyond 2^31 - 1 */
     QK_ELAUNCH = -3       /* the HIP runtime refused a launch */
 };

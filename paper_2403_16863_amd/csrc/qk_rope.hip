@@ -229,6 +229,14 @@ int check(int B, int N, int H, int Hkv, int d) {
 
 bool given(const qk_heads* t) { return t && t->data; }
 
+// An output that begins where another tensor does writes what other workgroups still read, or write.  Its own input's memory (`own`) with the
+// same strides is left to it: a lane reads a vector before it writes it.
+bool meets(const qk_heads* out, const qk_heads* other, bool own, int B, int N, int heads) {
+    if (!given(out) || !given(other) || out->data != other->data) return false;
+    return !own || (B > 1 && out->batch_stride != other->batch_stride) || (N > 1 && out->token_stride != other->token_stride) ||
+           (heads > 1 && out->head_stride != other->head_stride);
+}
+
 void strides(const qk_heads* t, long long* s) { s[0] = t->batch_stride, s[1] = t->token_stride, s[2] = t->head_stride; }
 
 template <bool BACK>
@@ -266,6 +274,10 @@ int qk_norm_rope(const qk_heads* q, const qk_heads* k, const qk_heads* q_out, co
         a.t[z].x = (const uint16_t*)in[z]->data, a.t[z].y = (uint16_t*)out[z]->data, a.t[z].w = w[z], a.t[z].heads = heads[z];
         strides(in[z], a.t[z].xs), strides(out[z], a.t[z].ys);
     }
+    for (int z = 0; z < 2; ++z)
+        for (int y = 0; y < 2; ++y)
+            if (heads[z] && meets(out[z], in[y], z == y, B, N, heads[z])) return QK_EINVAL;
+    if (meets(q_out, k_out, false, B, N, H)) return QK_EINVAL;
     const Grid g = grid_of((long long)B * N, H + Hkv, d, false);
     a.cos = cos, a.sin = sin, a.positions = positions, a.tokens = (long long)B * N, a.N = N, a.rows = rows, a.interleaved = interleaved;
     a.weight_f32 = weight_f32, a.head_step = g.head_step, a.blocks_y = g.y, a.eps = eps;
@@ -314,6 +326,10 @@ int qk_norm_rope_bwd(const qk_heads* dq_out, const qk_heads* dk_out, const qk_he
         a.t[z].dy = (const uint16_t*)dy[z]->data, a.t[z].y = (uint16_t*)dx[z]->data, a.t[z].w = w[z], a.t[z].heads = heads[z];
         strides(dy[z], a.t[z].dys), strides(dx[z], a.t[z].ys);
     }
+    for (int z = 0; z < 2; ++z)
+        for (int y = 0; y < 2; ++y)
+            if (heads[z] && (meets(dx[z], dy[y], z == y, B, N, heads[z]) || (w[y] && meets(dx[z], x[y], z == y, B, N, heads[z])))) return QK_EINVAL;
+    if (meets(dq, dk, false, B, N, H)) return QK_EINVAL;
     a.cos = cos, a.sin = sin, a.positions = positions, a.ws = sums ? (float*)workspace : nullptr, a.tokens = (long long)B * N, a.N = N;
     a.rows = rows, a.interleaved = interleaved, a.weight_f32 = weight_f32, a.head_step = g.head_step, a.blocks_y = g.y, a.eps = eps;
     void* list[] = {&a};
