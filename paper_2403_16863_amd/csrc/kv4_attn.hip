@@ -13,7 +13,7 @@
 //     each of two groups of 16, and the cache holds the values in quads of tokens for that reason.
 // Memory binds long calls: the loop reads 6.3 TB/s (64 sequences of up to 8192 keys); a launch's beginnings, ends and second kernel are the rest.
 // More rows (`wide_segment`): 128 or 256 a workgroup, tiles of 64 keys converted once into LDS, the next tile's scores multiplied during this one's
-// softmax.  The card's power binds it (1085 TFLOP/s for 2048 queries behind 14336 keys, 32 heads on 8, d = 128): its matrix instructions run at 2500
+// softmax.  The card's power binds it (1050 to 1100 TFLOP/s, by the card, for 2048 queries behind 14336 keys, 32 heads on 8, d = 128): its matrix instructions run at 2500
 // TFLOP/s on constant data, on random data at 1700, and at 1390 with a read of LDS, an exponential and four more vector instructions to each.
 //
 // All values of the cache are exact in binary16, so one kernel serves both types: bfloat16 queries become binary16 relative to
@@ -858,8 +858,8 @@ __device__ __forceinline__ void wide_segment(const AttnArgs& a, const Sequence& 
 }
 
 // The two forms of a segment: NT tiles of 16 rows with the keys shared out to NW waves, or 32 rows to each of NW waves in G groups.  In tiles: `begin`, what
-// it costs a workgroup to begin and end a segment (about 5 us; 0, 4, 8, 16 tiles: 64 sequences of up to 8192 keys 80, 76, 74.5, 74.3 us, 8 of up to
-// 4000 19.2, 16.6, 15.5, 15.4); `least`, the shortest range; `whole`, up to which a segment is left whole if no other is longer.
+// it costs a workgroup to begin and end a segment (about 5 us; 0, 4, 8, 16 tiles: 64 sequences of up to 8192 keys 75.4, 72.7, 71.7, 72.0 us, 8 of up to
+// 4000 18.6, 15.6, 14.8, 14.8); `least`, the shortest range; `whole`, up to which a segment is left whole if no other is longer.
 template <int D, int NT, int NW, bool BF>
 struct Narrow {
     static constexpr int rows = 16 * NT, tile = kTile, waves_simd = NT == 1 ? 4 : 2, threads = 64 * NW;
@@ -1022,17 +1022,17 @@ struct Choice {
 };
 
 // Both sides of the choices, in us (bfloat16, d = 128, 32 heads on 8 unless said; forms timed in turn on one card):
-//  * rows from 33 on in the wide form, not four tiles of 16 rows a wave: 40 rows over four caches of up to 20000 keys 39 against 73, 64 over the
-//    same 30 against 52.  24 rows: 33 against 34 in two tiles of 16, with d = 64 29 against 26.
-//  * kRanges: 768, 1024, 1536, 2048 ranges: 64 sequences of up to 8192 keys 83, 80, 83, 82; two of up to 131072 40, 42, 47, 49.  Eight waves a workgroup
-//    and half the ranges: 87 and 40.
-//    Forms of which two workgroups fill a unit, 1024 and 512: 24 rows over 16 caches of up to 6000 keys 34, 26, the same of 32 rows, d = 64, 26, 21.5.
+//  * rows from 33 on in the wide form, not four tiles of 16 rows a wave: 40 rows over four caches of up to 20000 keys 39 against 58, 64 over the
+//    same 31 against 53.  Up to 32 in two tiles of 16: 24 rows over 16 caches of up to 6000 keys 26.4 against 31.0, 32 rows, d = 64, 21.4 against 24.4.
+//  * kRanges: 768, 1024, 1536, 2048 ranges: 64 sequences of up to 8192 keys 70, 72, 76, 75; two of up to 131072 36.5, 37.6, 43, 44; but with 3/4 of the ranges, so
+//    of the units, the other forms take 5 to 21 % longer (the chunk below 582 against 481).  Eight waves a workgroup and half the ranges: 72.5 and 36.7.
+//    Forms of which two workgroups fill a unit, 1024 and 512: 24 rows over 16 caches of up to 6000 keys 33.7, 26.4, 32 rows, d = 64, 25.8, 21.4.
 //  * kMany: 256 rows a workgroup instead of 128 halve the conversions, but twice as many rows begin and end together: 2048 queries behind 14336 keys
-//    497 against 475, 300 behind 12000, 16 heads on 4, d = 64, 62 against 59 (1200 rows), 150 behind 12000 82 against 83.5 (600 rows); caches of 2048 keys, which
-//    are not cut, 52 against 61.
-//  * kPaired: one prompt of 1500, 12 heads on 4, d = 64, 22.3 against 26.2, eight times 100 queries over 2000 keys 37 against 43 (256 row blocks), three prompts of
-//    1500 (432) 29.1 against 28.6, two of 32 heads (752) 65 against 53.  Of 200 keys, four tiles, 11.5 against 10.4: from 512 on.
-//  * kShort: caches of 1500 keys cut all the same: 64 sequences 23 against 20, one of 1003 keys 11.7 against 10.9 with its 16 waves, prompts 39 against 31.
+//    515 against 485, 300 behind 12000, 16 heads on 4, d = 64, 59 against 58 (1200 rows), 150 behind 12000 83 against 84 (600 rows); caches of 2048 keys, which
+//    are not cut, 51 against 61.
+//  * kPaired: one prompt of 1500, 12 heads on 4, d = 64, 22.7 against 26.6, eight times 100 queries over 2000 keys 37.6 against 43.8 (256 row blocks), three prompts of
+//    1500 (432) 29.7 against 29.0, two of 32 heads (752) 66 against 55.  Of 200 keys, four tiles, 11.6 against 10.6: from 512 on.
+//  * kShort: caches of 1500 keys cut all the same: 64 sequences 23 against 19, one of 1003 keys 11.5 against 10.7 with its 16 waves, one prompt 32 against 23, three 55 against 29.
 constexpr int kShort = 2048;   // keys up to which nothing is cut
 constexpr int kMany = 1024;    // rows of a sequence and head from which 256 of them share a tile's conversion
 constexpr int kPaired = 256;   // row blocks up to which two groups of waves share one: a workgroup to each unit
