@@ -276,8 +276,8 @@ int qk_norm_rope(const qk_heads* q, const qk_heads* k, const qk_heads* q_out, co
     }
     for (int z = 0; z < 2; ++z)
         for (int y = 0; y < 2; ++y)
-            if (heads[z] && meets(out[z], in[y], z == y, B, N, heads[z])) return QK_EINVAL;
-    if (meets(q_out, k_out, false, B, N, H)) return QK_EINVAL;
+            if (heads[z] && heads[y] && meets(out[z], in[y], z == y, B, N, heads[z])) return QK_EINVAL;
+    if (H && Hkv && meets(q_out, k_out, false, B, N, H)) return QK_EINVAL;
     const Grid g = grid_of((long long)B * N, H + Hkv, d, false);
     a.cos = cos, a.sin = sin, a.positions = positions, a.tokens = (long long)B * N, a.N = N, a.rows = rows, a.interleaved = interleaved;
     a.weight_f32 = weight_f32, a.head_step = g.head_step, a.blocks_y = g.y, a.eps = eps;
@@ -328,8 +328,8 @@ int qk_norm_rope_bwd(const qk_heads* dq_out, const qk_heads* dk_out, const qk_he
     }
     for (int z = 0; z < 2; ++z)
         for (int y = 0; y < 2; ++y)
-            if (heads[z] && (meets(dx[z], dy[y], z == y, B, N, heads[z]) || (w[y] && meets(dx[z], x[y], z == y, B, N, heads[z])))) return QK_EINVAL;
-    if (meets(dq, dk, false, B, N, H)) return QK_EINVAL;
+            if (heads[z] && heads[y] && (meets(dx[z], dy[y], z == y, B, N, heads[z]) || (w[y] && meets(dx[z], x[y], z == y, B, N, heads[z])))) return QK_EINVAL;
+    if (H && Hkv && meets(dq, dk, false, B, N, H)) return QK_EINVAL;
     a.cos = cos, a.sin = sin, a.positions = positions, a.ws = sums ? (float*)workspace : nullptr, a.tokens = (long long)B * N, a.N = N;
     a.rows = rows, a.interleaved = interleaved, a.weight_f32 = weight_f32, a.head_step = g.head_step, a.blocks_y = g.y, a.eps = eps;
     void* list[] = {&a};

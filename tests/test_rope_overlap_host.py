@@ -12,8 +12,8 @@ def h(data, batch=4096, token=256, head=64):
     return rope.Heads(data, batch, token, head)
 
 
-def forward(q=h(0x10000), k=h(0x20000), qo=h(0x30000), ko=h(0x40000), B=2, N=3, H=4):
-    return rope.lib().qk_norm_rope(q, k, qo, ko, None, None, 0, p(0x60000), p(0x70000), p(0x80000), 9, 1e-6, 0, B, N, H, 2, 64, 0, None)
+def forward(q=h(0x10000), k=h(0x20000), qo=h(0x30000), ko=h(0x40000), B=2, N=3, H=4, Hkv=2):
+    return rope.lib().qk_norm_rope(q, k, qo, ko, None, None, 0, p(0x60000), p(0x70000), p(0x80000), 9, 1e-6, 0, B, N, H, Hkv, 64, 0, None)
 
 
 def backward(dqo=h(0x10000), dko=h(0x20000), q=h(0x30000), k=h(0x40000), dq=h(0x50000), dk=h(0x58000)):
@@ -39,4 +39,5 @@ def test_in_place_is_not_refused_for_it():
         return                                                     # the addresses are nobody's
     assert forward(qo=h(0x10000)) == rope.QK_ELAUNCH
     assert forward(qo=h(0x10000, batch=0, token=8), B=1, N=1) == rope.QK_ELAUNCH       # strides of a size of 1 are not looked at
+    assert forward(k=h(0x30000), ko=h(0x30000), Hkv=0) == rope.QK_ELAUNCH              # nor is a tensor of no heads
     assert backward(dq=h(0x10000), dk=h(0x20000)) == rope.QK_ELAUNCH
