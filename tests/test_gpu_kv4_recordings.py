@@ -125,3 +125,49 @@ def test_attention_in_a_graph_of_torch_is_cut_as_it_is_without(plain, pool):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+
+
+@pytest.mark.parametrize("which", ["own", "default"])
+def test_calls_beside_a_recording_of_torch_in_another_thread(which):
+    """They take memory of their own streams, and end neither the recording nor themselves."""
+    import threading
+
+    from paper_2403_16863_amd import kv4, rope
+    s = setup(([5000, 30], [1, 1], 8, 2, 128, 16, True), torch.float16)
+    out, lse = torch.empty_like(s["q"]), torch.empty(s["q"].shape[:2], device="cuda")
+    q, _, dqo, _, (qw, _), c, sn, positions = inputs(1, 600, 4, 2, 64, torch.float16, torch.float16)
+    dq, dw = torch.empty(1, 600, 4, 64, dtype=torch.float16, device="cuda"), torch.empty(64, device="cuda")
+
+    def calls():
+        kv4.kv4_attn(s["q"], s["cache"], s["tables"], s["lens"], out, lse, True, s["scale"], s["cu"], 1)
+        rope.qk_norm_rope_bwd(dqo, None, q, None, dq, None, c, sn, positions, qw, None, dw, None)
+    calls()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in (out, lse, dq, dw)]
+    for t in (out, lse, dq, dw):
+        t.zero_()
+    errors = []
+
+    def beside():
+        try:
+            with torch.cuda.stream(torch.cuda.Stream() if which == "own" else torch.cuda.default_stream()):
+                calls()
+        except Exception as e:
+            errors.append(e)
+    x, y = torch.arange(8.0, device="cuda"), torch.zeros(8, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        torch.add(x, 1, out=y)
+        thread = threading.Thread(target=beside)
+        thread.start()
+        thread.join()
+        y.mul_(2)
+    assert not errors
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip((out, lse, dq, dw), want))
+    for _ in range(3):
+        y.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, 2 * (x + 1))
