@@ -1,0 +1,422 @@
+// Host side of the linear layers' products (include/linear.h): checks, choice of the tile, launches; and the small kernels around
+// the products of linear_kernel.h: the joining of parts, and the activation's backward step.
+#include "../../include/linear.h"
+
+#include <limits.h>
+
+#include "linear_tiles.h"
+#include "memory_check.h"
+
+namespace linear {
+
+// C from the parts of the ranges of k, in range order, with the epilogue; a thread for eight consecutive elements.
+template <class T>
+__global__ __launch_bounds__(64) void join_kernel(const float* parts, Args p, int ranges, unsigned chunks) {
+    const unsigned i = blockIdx.x * 64 + threadIdx.x;
+    if (i >= chunks) return;
+    const f32x4* src = reinterpret_cast<const f32x4*>(parts) + (size_t)i * 2;
+    f32x4 x = src[0], y = src[1];
+#pragma unroll 4
+    for (int r = 1; r < ranges; ++r) {
+        src += (size_t)chunks * 2;
+        x += src[0];
+        y += src[1];
+    }
+    float v[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+    const unsigned row = (unsigned)p.N / 8, m = i / row;
+    finish8<T>(p.e, (uint16_t*)p.out, p.ldo, (int)m, (int)(i - m * row) * 8, v);
+}
+
+// dz = dy act'(pre), rounded, and the rows' sums for dbias, in one pass over dy and pre: memory binds.  A workgroup has 256 / lanes rows of `lanes` vectors of 8
+// columns (a power of two, 64 at most) and goes through a chunk of the rows; its sums meet in LDS in a fixed order.
+struct SlopeArgs {
+    const uint16_t *dy, *pre;
+    uint16_t* dz;
+    float* sums;  // [chunk][N], or null
+    long long lddy, ldpre;
+    int M, N, rows, lanes, act;
+};
+
+template <class T>
+__global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a) {
+    __shared__ float part[256 * 9];
+    const int lane = threadIdx.x % a.lanes, at = threadIdx.x / a.lanes, step = 256 / a.lanes;
+    const int n = (blockIdx.x * a.lanes + lane) * 8;
+    const long long first = (long long)blockIdx.y * a.rows, end = min((long long)a.M, first + a.rows);
+    float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (n < a.N) {
+        const uint16_t *dy = a.dy + n, *pre = a.pre + n;
+#pragma unroll 4
+        for (long long m = first + at; m < end; m += step) {
+            float g[8], v[8];
+            unpack8<T>(*(const u32x4*)(dy + m * a.lddy), g);
+            if (a.act) {
+                unpack8<T>(*(const u32x4*)(pre + m * a.ldpre), v);
+                act_slope8(v, g, a.act);
+                if (a.dz) *(u32x4*)(a.dz + m * a.N + n) = pack8<T>(g);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] += g[i];
+        }
+    }
+    if (!a.sums) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) part[threadIdx.x * 9 + i] = sum[i];
+    __syncthreads();
+    for (int c = threadIdx.x; c < a.lanes * 8; c += 256) {
+        float t = 0;
+        for (int r = 0; r < step; ++r) t += part[(r * a.lanes + c / 8) * 9 + c % 8];
+        const int column = blockIdx.x * a.lanes * 8 + c;
+        if (column < a.N) a.sums[(size_t)blockIdx.y * a.N + column] = t;
+    }
+}
+
+// dbias from the chunks' sums: 32 columns a workgroup, 8 threads to a column.
+__global__ __launch_bounds__(256) void bias_kernel(const float* sums, int chunks, int N, float* dbias) {
+    __shared__ float part[256];
+    const int c = blockIdx.x * 32 + threadIdx.x % 32;
+    float t = 0;
+    if (c < N) {
+#pragma unroll 8
+        for (int i = threadIdx.x / 32; i < chunks; i += 8) t += sums[(size_t)i * N + c];
+    }
+    part[threadIdx.x] = t;
+    __syncthreads();
+    if (threadIdx.x >= 32 || c >= N) return;
+#pragma unroll
+    for (int i = 1; i < 8; ++i) t += part[threadIdx.x + 32 * i];
+    dbias[c] = t;
+}
+
+// ---- choice of the tile.  With n tiles on the busiest of the 256 units, and f of the units' n rounds filled, a product takes about
+//     ceil(K / kstage) * max(ceil(n / occ) * alone, n * full) * (1 + load * f) + n * ends + 2.7     (us)
+// and in ranges of k a second launch and the parts' way through memory in addition.
+struct Shape {
+    int bm, bn, bk, wk, threads, occ;
+    float alone, full, load, ends;
+};
+template <int I>
+constexpr Shape shape(float alone, float full, float load, float ends) {
+    using T = TileOf<I>;
+    return {T::BM, T::BN, T::BK, T::WK, T::WM * T::WN * T::WK * 64, T::OCC, alone, full, load, ends};
+}
+static constexpr Shape kShapes[kTiles] = {
+    shape<0>(0.60f, 0.f, 0.3f, 0.5f),      shape<1>(0.229f, 0.288f, 0.06f, 0.11f), shape<2>(0.215f, 0.181f, 0.25f, 0.f),
+    shape<3>(0.310f, 0.f, 0.61f, 0.37f),   shape<4>(0.327f, 0.f, 0.62f, 1.02f),    shape<5>(0.579f, 0.395f, 0.39f, 0.41f),
+    shape<6>(0.443f, 0.f, 0.56f, 1.83f),   shape<7>(0.502f, 0.f, 0.80f, 2.39f),    shape<8>(0.768f, 0.f, 0.77f, 2.94f),
+    shape<9>(0.982f, 0.f, 0.66f, 4.20f)};
+
+constexpr long long kUnits = 256, kPartBytes = 64ll << 20;
+constexpr int kMostRanges = 32;
+
+struct Plan {
+    int tile, ranges, kc;
+    long long bytes;  // of the parts
+};
+
+static long long tiles_of(const Shape& s, int M, int N) { return (long long)(1 + (M - 1) / s.bm) * (1 + (N - 1) / s.bn); }
+static bool fits(const Shape& s, int M, int N, int ranges) { return tiles_of(s, M, N) * ranges * s.threads <= (long long)UINT_MAX; }
+
+static Plan plan_of(int tile, int M, int N, int K, int ranges) {
+    const Shape& s = kShapes[tile];
+    const int step = s.bk * s.wk;
+    const int kc = (int)(((long long)K + ranges - 1) / ranges + step - 1) / step * step;
+    ranges = (int)(((long long)K + kc - 1) / kc);
+    return {tile, ranges, kc, ranges > 1 ? 4ll * ranges * M * N : 0};
+}
+
+static float time_of(const Shape& s, int M, int N, int K, int ranges, int kc) {
+    const long long tiles = tiles_of(s, M, N) * ranges, n = (tiles + kUnits - 1) / kUnits;
+    const long long stages = ((long long)(ranges > 1 ? kc : K) + s.bk * s.wk - 1) / (s.bk * s.wk);
+    const float alone = (float)((n + s.occ - 1) / s.occ) * s.alone, full = (float)n * s.full, filled = (float)tiles / (float)(n * kUnits);
+    const float us = (float)stages * (alone > full ? alone : full) * (1.f + s.load * filled) + (float)n * s.ends + 2.7f;
+    return ranges > 1 ? us + 2.3f + 0.4e-6f * 4.f * (float)ranges * (float)M * (float)N : us;
+}
+
+static Plan choose(int M, int N, int K, int layout, bool memory) {
+    Plan best = {-1, 1, K, 0};
+    float best_us = 0;
+    for (int t = 0; t < kTiles; ++t) {
+        const Shape& s = kShapes[t];
+        if (!fits(s, M, N, 1)) continue;
+        const long long tiles = tiles_of(s, M, N);
+        for (int r = 1; r <= kMostRanges; ++r) {
+            if (r > 1 && (!memory || tiles * r > kUnits * s.occ || (long long)r * 256 > K)) break;
+            const Plan p = plan_of(t, M, N, K, r);
+            if (p.ranges != r || p.bytes > kPartBytes) continue;
+            const float us = time_of(s, M, N, K, r, p.kc);
+            if (best.tile < 0 || us < best_us) best = p, best_us = us;
+        }
+    }
+    return best;
+}
+
+static const void* kernel_of(int layout, int dtype, int tile, bool parts) {
+    if (layout == ROWS) return dtype ? product_of<ROWS, true>(tile, parts) : product_of<ROWS, false>(tile, parts);
+    if (layout == ROWS_N) return dtype ? product_of<ROWS_N, true>(tile, parts) : product_of<ROWS_N, false>(tile, parts);
+    return dtype ? product_of<TOKENS, true>(tile, parts) : product_of<TOKENS, false>(tile, parts);
+}
+
+static int launch(const void* fn, dim3 grid, int threads, void** args, void* stream) {
+    if (hipLaunchKernel(fn, grid, dim3(threads), args, 0, (hipStream_t)stream) == hipSuccess) return LINEAR_OK;
+    (void)hipGetLastError();
+    return LINEAR_ELAUNCH;
+}
+
+static int run(const Plan& plan, int layout, int dtype, Args a, void* workspace, void* stream) {
+    const Shape& s = kShapes[plan.tile];
+    const bool parts = plan.ranges > 1;
+    Args product = a;
+    product.kc = plan.kc;
+    if (parts) product.out = (char*)workspace;
+    void* args[] = {&product};
+    const int rc = launch(kernel_of(layout, dtype, plan.tile, parts), dim3((unsigned)(tiles_of(s, a.M, a.N) * plan.ranges)), s.threads, args, stream);
+    if (rc || !parts) return rc;
+    const float* from = (const float*)workspace;
+    int ranges = plan.ranges;
+    unsigned chunks = (unsigned)((long long)a.M * a.N / 8);
+    void* join[] = {&from, &a, &ranges, &chunks};
+    return launch(dtype ? (const void*)join_kernel<BF16> : (const void*)join_kernel<F16>, dim3((chunks + 63) / 64), 64, join, stream);
+}
+
+// ---- checks
+constexpr int kMost = 1 << 22, kMostRows = 1 << 30;
+
+static bool given(const linear_rows* t) { return t && t->data; }
+
+static int check_sizes(int M, int N, int K, int dtype, int activation) {
+    if (M < 1 || N < 8 || K < 8 || N % 8 || K % 8 || (dtype != LINEAR_F16 && dtype != LINEAR_BF16) || activation < LINEAR_NONE ||
+        activation > LINEAR_GELU_TANH)
+        return LINEAR_EINVAL;
+    return M > kMostRows || N > kMost || K > kMost ? LINEAR_EUNSUPPORTED : LINEAR_OK;
+}
+
+static int check_matrix(const linear_rows* t, int rows, int columns) {
+    if (!given(t) || (uintptr_t)t->data % 16) return LINEAR_EINVAL;
+    if (rows == 1) return LINEAR_OK;
+    if (t->stride % 8 || t->stride < columns) return LINEAR_EINVAL;
+    return t->stride > kMost ? LINEAR_EUNSUPPORTED : LINEAR_OK;
+}
+
+static int stride_of(const linear_rows* t, int rows, int columns) { return rows > 1 ? (int)t->stride : columns; }
+static Rows2D block(const linear_rows* t, int rows, int columns) { return {given(t) ? t->data : nullptr, rows, columns, given(t) ? t->stride : 0}; }
+static Rows2D vector_of(const void* p, long long bytes) { return {p, 1, bytes / 2, 0}; }
+
+static long long up(long long bytes) { return (bytes + 255) / 256 * 256; }
+
+// Workgroups of the activation's backward step: 1024 where there are rows enough for them to have two passes each.
+struct SlopeGrid {
+    int lanes, blocks, rows, chunks;
+};
+static SlopeGrid slope_grid(int M, int N) {
+    SlopeGrid g;
+    g.lanes = 1;
+    while (g.lanes < 64 && g.lanes * 8 < N) g.lanes *= 2;
+    g.blocks = (N + g.lanes * 8 - 1) / (g.lanes * 8);
+    const int pass = 256 / g.lanes;
+    const long long most = (M + 2ll * pass - 1) / (2 * pass), want = g.blocks >= 1024 ? 1 : 1024 / g.blocks;
+    const long long chunks = want < most ? want : most;
+    g.rows = (int)(((M + chunks - 1) / chunks + pass - 1) / pass * pass);
+    g.chunks = (int)(((long long)M + g.rows - 1) / g.rows);
+    return g;
+}
+
+struct Backward {
+    Plan dx, dw;
+    SlopeGrid slope;
+    int dx_layout;
+    long long dz, sums, parts;  // bytes
+    long long total() const { return dz + sums + parts; }
+};
+// dx = dz w^T: of a weight of K rows both operands have the products' index, N, along their rows.  dw: the tokens are the index; the
+// product is dw itself or, of N rows, its transpose.
+static Backward backward_of(int M, int N, int K, int w_rows_of_n, int dw_rows_of_n, int activation, bool dx, bool dw, bool dbias) {
+    Backward b = {};
+    b.slope = slope_grid(M, N);
+    b.dx_layout = w_rows_of_n ? ROWS : ROWS_N;
+    if (dx) b.dx = choose(M, K, N, b.dx_layout, true);
+    if (dw) b.dw = dw_rows_of_n ? choose(N, K, M, TOKENS, true) : choose(K, N, M, TOKENS, true);
+    b.dz = activation && (dx || dw) ? up(2ll * M * N) : 0;
+    b.sums = dbias ? up(4ll * b.slope.chunks * N) : 0;
+    b.parts = b.dx.bytes > b.dw.bytes ? b.dx.bytes : b.dw.bytes;
+    return b;
+}
+
+}  // namespace linear
+
+extern "C" {
+
+long long gemm_linear_workspace(int M, int N, int K, int w_rows_of_n) {
+    using namespace linear;
+    if (const int rc = check_sizes(M, N, K, LINEAR_F16, LINEAR_NONE)) return rc;
+    const Plan p = choose(M, N, K, w_rows_of_n ? ROWS_N : ROWS, true);
+    return p.tile < 0 ? LINEAR_EUNSUPPORTED : p.bytes;
+}
+
+int gemm_linear(const linear_rows* x, const linear_rows* w, int w_rows_of_n, const void* bias, int bias_f32, const linear_rows* residual,
+                const linear_rows* pre, const linear_rows* out, int activation, int M, int N, int K, int dtype, void* workspace,
+                long long workspace_bytes, void* stream) {
+    using namespace linear;
+    if (const int rc = check_sizes(M, N, K, dtype, activation)) return rc;
+    const int wr = w_rows_of_n ? N : K, wc = w_rows_of_n ? K : N;
+    if (const int rc = check_matrix(x, M, K)) return rc;
+    if (const int rc = check_matrix(w, wr, wc)) return rc;
+    if (const int rc = check_matrix(out, M, N)) return rc;
+    if (given(residual))
+        if (const int rc = check_matrix(residual, M, N)) return rc;
+    if (given(pre))
+        if (const int rc = check_matrix(pre, M, N)) return rc;
+    if ((uintptr_t)bias % 16 || (uintptr_t)workspace % 16) return LINEAR_EINVAL;
+    const Rows2D xs = block(x, M, K), ws = block(w, wr, wc), bs = vector_of(bias, (long long)N * (bias_f32 ? 4 : 2)), rs = block(residual, M, N);
+    const Rows2D os = block(out, M, N), ps = block(pre, M, N);
+    const bool in_place = given(residual) && residual->data == out->data && (M == 1 || residual->stride == out->stride);
+    if (rows_meet(os, xs) || rows_meet(os, ws) || rows_meet(os, bs) || (!in_place && rows_meet(os, rs)) || rows_meet(os, ps)) return LINEAR_EINVAL;
+    if (rows_meet(ps, xs) || rows_meet(ps, ws) || rows_meet(ps, bs) || rows_meet(ps, rs)) return LINEAR_EINVAL;
+    const int layout = w_rows_of_n ? ROWS_N : ROWS;
+    Plan plan = choose(M, N, K, layout, true);
+    if (plan.tile < 0) return LINEAR_EUNSUPPORTED;
+    if (plan.bytes) {
+        if (!workspace || workspace_bytes < plan.bytes) {
+            plan = choose(M, N, K, layout, false);
+        } else {
+            const Rows2D mine = vector_of(workspace, plan.bytes);
+            for (const Rows2D& t : {xs, ws, bs, rs, os, ps})
+                if (rows_meet(mine, t)) return LINEAR_EINVAL;
+        }
+    }
+    Args a = {};
+    a.a = (const char*)x->data, a.b = (const char*)w->data, a.out = (char*)out->data, a.M = M, a.N = N, a.K = K;
+    a.lda = stride_of(x, M, K), a.ldb = stride_of(w, wr, wc), a.ldo = stride_of(out, M, N);
+    a.e.bias = bias, a.e.bias_f32 = bias_f32, a.e.act = activation;
+    if (given(residual)) a.e.residual = (const uint16_t*)residual->data, a.e.ldr = stride_of(residual, M, N);
+    if (given(pre)) a.e.pre = (uint16_t*)pre->data, a.e.ldp = stride_of(pre, M, N);
+    return run(plan, layout, dtype, a, workspace, stream);
+}
+
+long long gemm_linear_bwd_workspace(int M, int N, int K, int w_rows_of_n, int dw_rows_of_n, int activation, int dx, int dw, int dbias) {
+    using namespace linear;
+    if (const int rc = check_sizes(M, N, K, LINEAR_F16, activation)) return rc;
+    if (!dx && !dw && !dbias) return LINEAR_EINVAL;
+    const Backward b = backward_of(M, N, K, w_rows_of_n, dw_rows_of_n, activation, dx, dw, dbias);
+    return b.dx.tile < 0 || b.dw.tile < 0 ? LINEAR_EUNSUPPORTED : b.total();
+}
+
+int gemm_linear_bwd(const linear_rows* dy, const linear_rows* x, const linear_rows* w, int w_rows_of_n, const linear_rows* pre,
+                    const linear_rows* dx, const linear_rows* dw, int dw_rows_of_n, float* dbias, int activation, int M, int N, int K,
+                    int dtype, void* workspace, long long workspace_bytes, void* stream) {
+    using namespace linear;
+    if (const int rc = check_sizes(M, N, K, dtype, activation)) return rc;
+    const bool want_x = given(dx), want_w = given(dw);
+    if (!want_x && !want_w && !dbias) return LINEAR_EINVAL;
+    const int wr = w_rows_of_n ? N : K, wc = w_rows_of_n ? K : N, dwr = dw_rows_of_n ? N : K, dwc = dw_rows_of_n ? K : N;
+    if (const int rc = check_matrix(dy, M, N)) return rc;
+    if (activation)
+        if (const int rc = check_matrix(pre, M, N)) return rc;
+    if (want_x) {
+        if (const int rc = check_matrix(w, wr, wc)) return rc;
+        if (const int rc = check_matrix(dx, M, K)) return rc;
+    }
+    if (want_w) {
+        if (const int rc = check_matrix(x, M, K)) return rc;
+        if (const int rc = check_matrix(dw, dwr, dwc)) return rc;
+    }
+    if ((uintptr_t)dbias % 16 || (uintptr_t)workspace % 16) return LINEAR_EINVAL;
+    const Backward b = backward_of(M, N, K, w_rows_of_n, dw_rows_of_n, activation, want_x, want_w, dbias);
+    if (b.dx.tile < 0 || b.dw.tile < 0 || (long long)b.slope.blocks * b.slope.chunks * 256 > (long long)UINT_MAX || b.slope.chunks > 65535)
+        return LINEAR_EUNSUPPORTED;
+    if (b.total() && (!workspace || workspace_bytes < b.total())) return LINEAR_EINVAL;
+    const Rows2D in[] = {block(dy, M, N), activation ? block(pre, M, N) : Rows2D{}, want_w ? block(x, M, K) : Rows2D{},
+                         want_x ? block(w, wr, wc) : Rows2D{}};
+    const Rows2D out[] = {want_x ? block(dx, M, K) : Rows2D{}, want_w ? block(dw, dwr, dwc) : Rows2D{}, vector_of(dbias, 4ll * N),
+                          b.total() ? vector_of(workspace, b.total()) : Rows2D{}};
+    for (int i = 0; i < 4; ++i) {
+        for (const Rows2D& t : in)
+            if (rows_meet(out[i], t)) return LINEAR_EINVAL;
+        for (int j = 0; j < i; ++j)
+            if (rows_meet(out[i], out[j])) return LINEAR_EINVAL;
+    }
+    char* const dz = (char*)workspace;
+    float* const sums = (float*)(dz + b.dz);
+    void* const parts = dz + b.dz + b.sums;
+    if (b.dz || dbias) {
+        SlopeArgs s = {};
+        s.dy = (const uint16_t*)dy->data, s.lddy = stride_of(dy, M, N), s.M = M, s.N = N, s.rows = b.slope.rows, s.lanes = b.slope.lanes, s.act = activation;
+        s.pre = s.dy;
+        if (activation) s.pre = (const uint16_t*)pre->data, s.ldpre = stride_of(pre, M, N);
+        if (b.dz) s.dz = (uint16_t*)dz;
+        if (dbias) s.sums = sums;
+        void* args[] = {&s};
+        if (const int rc = launch(dtype ? (const void*)slope_kernel<BF16> : (const void*)slope_kernel<F16>, dim3(b.slope.blocks, b.slope.chunks), 256, args, stream))
+            return rc;
+        if (dbias) {
+            const float* from = sums;
+            int chunks = b.slope.chunks;
+            void* list[] = {&from, &chunks, &N, &dbias};
+            if (const int rc = launch((const void*)bias_kernel, dim3((N + 31) / 32), 256, list, stream)) return rc;
+        }
+    }
+    const char* const g = b.dz ? dz : (const char*)dy->data;
+    const int ldg = b.dz ? N : stride_of(dy, M, N);
+    if (want_x) {
+        Args a = {};
+        a.a = g, a.lda = ldg, a.b = (const char*)w->data, a.ldb = stride_of(w, wr, wc), a.out = (char*)dx->data, a.ldo = stride_of(dx, M, K);
+        a.M = M, a.N = K, a.K = N;
+        if (const int rc = run(b.dx, b.dx_layout, dtype, a, parts, stream)) return rc;
+    }
+    if (want_w) {
+        Args a = {};
+        a.a = (const char*)x->data, a.lda = stride_of(x, M, K), a.b = g, a.ldb = ldg, a.M = K, a.N = N, a.K = M;
+        if (dw_rows_of_n) a.b = (const char*)x->data, a.ldb = stride_of(x, M, K), a.a = g, a.lda = ldg, a.M = N, a.N = K;
+        a.out = (char*)dw->data, a.ldo = stride_of(dw, dwr, dwc);
+        if (const int rc = run(b.dw, TOKENS, dtype, a, parts, stream)) return rc;
+    }
+    return LINEAR_OK;
+}
+
+int linear_num_tiles(void) { return linear::kTiles; }
+
+int linear_choice(int M, int N, int K, int layout, int* tile, int* ranges) {
+    using namespace linear;
+    if (M < 1 || N < 8 || K < 1 || N % 8 || layout < ROWS || layout > TOKENS || !tile || !ranges || (layout == TOKENS ? M % 8 : K % 8)) return LINEAR_EINVAL;
+    if (N > kMost || (layout == TOKENS ? M > kMost || K > kMostRows : K > kMost || M > kMostRows)) return LINEAR_EUNSUPPORTED;
+    const Plan p = choose(M, N, K, layout, true);
+    if (p.tile < 0) return LINEAR_EUNSUPPORTED;
+    *tile = p.tile, *ranges = p.ranges;
+    return LINEAR_OK;
+}
+
+int linear_product(const linear_rows* a, const linear_rows* b, int layout, const linear_rows* c, int M, int N, int K, int dtype, int tile,
+                   int ranges, void* workspace, long long workspace_bytes, void* stream) {
+    using namespace linear;
+    int chosen, most;
+    if (const int rc = linear_choice(M, N, K, layout, &chosen, &most)) return rc;
+    if ((dtype != LINEAR_F16 && dtype != LINEAR_BF16) || tile < 0 || tile >= kTiles || ranges < 1 || ranges > kMostRanges || (uintptr_t)workspace % 16)
+        return LINEAR_EINVAL;
+    const int ar = layout == TOKENS ? K : M, ac = layout == TOKENS ? M : K, br = layout == ROWS_N ? N : K, bc = layout == ROWS_N ? K : N;
+    if (const int rc = check_matrix(a, ar, ac)) return rc;
+    if (const int rc = check_matrix(b, br, bc)) return rc;
+    if (const int rc = check_matrix(c, M, N)) return rc;
+    const Plan plan = plan_of(tile, M, N, K, ranges);
+    if (!fits(kShapes[tile], M, N, plan.ranges) || (plan.bytes && (long long)M * N / 8 > INT_MAX)) return LINEAR_EUNSUPPORTED;
+    if (plan.bytes && (!workspace || workspace_bytes < plan.bytes)) return LINEAR_EINVAL;
+    const Rows2D cs = block(c, M, N), mine = plan.bytes ? vector_of(workspace, plan.bytes) : Rows2D{};
+    for (const Rows2D& t : {block(a, ar, ac), block(b, br, bc)})
+        if (rows_meet(cs, t) || rows_meet(mine, t)) return LINEAR_EINVAL;
+    if (rows_meet(mine, cs)) return LINEAR_EINVAL;
+    Args p = {};
+    p.a = (const char*)a->data, p.b = (const char*)b->data, p.out = (char*)c->data, p.M = M, p.N = N, p.K = K;
+    p.lda = stride_of(a, ar, ac), p.ldb = stride_of(b, br, bc), p.ldo = stride_of(c, M, N);
+    return run(plan, layout, dtype, p, workspace, stream);
+}
+
+const char* linear_strerror(int code) {
+    switch (code) {
+        case LINEAR_OK: return "ok";
+        case LINEAR_EINVAL: return "invalid argument";
+        case LINEAR_EUNSUPPORTED: return "unsupported size";
+        case LINEAR_ELAUNCH: return "the HIP runtime refused the launch";
+        default: return "unknown error";
+    }
+}
+
+}  // extern "C"

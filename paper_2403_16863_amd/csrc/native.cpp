@@ -18,6 +18,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "../../include/kv4.h"
+#include "../../include/linear.h"
 #include "../../include/qk_rope.h"
 
 namespace {
@@ -38,6 +39,10 @@ decltype(&kv4_attn_workspace) g_kv4_attn_workspace = nullptr;
 decltype(&qk_norm_rope) g_rope = nullptr;
 decltype(&qk_norm_rope_bwd) g_rope_bwd = nullptr;
 decltype(&qk_norm_rope_bwd_workspace) g_rope_bwd_workspace = nullptr;
+decltype(&gemm_linear) g_linear = nullptr;
+decltype(&gemm_linear_workspace) g_linear_workspace = nullptr;
+decltype(&gemm_linear_bwd) g_linear_bwd = nullptr;
+decltype(&gemm_linear_bwd_workspace) g_linear_bwd_workspace = nullptr;
 
 // Whether torch's allocator has an address in a pool of its own: one that it opened for a graph that it records (or its user for tensors).  It looks
 // through all segments, which a recording can wait for.
@@ -426,6 +431,114 @@ PyObject* norm_rope_bwd(PyObject* const* args, Py_ssize_t nargs) {
     return PyLong_FromLong(rc);
 }
 
+// Linear layers: matrices of one type and device, with rows of any stride.
+
+struct LinearArgs {
+    Reader& r;
+    at::ScalarType type;
+    explicit LinearArgs(Reader& reader, PyObject* first) : r(reader), type(at::ScalarType::Undefined) {
+        if (THPVariable_Check(first) && THPVariable_Unpack(first).defined()) type = THPVariable_Unpack(first).scalar_type();
+    }
+    int dtype() const { return type == at::kHalf ? 0 : type == at::kBFloat16 ? 1 : -1; }
+    // [rows, columns] (each set by the first matrix that has it, 0 before), columns on end; None: left out.
+    linear_rows matrix(PyObject* o, int* rows, int* columns) {
+        if (o == Py_None) return {nullptr, 0};
+        const at::Tensor* t = r.strided(o, 2);
+        return t ? sized(*t, rows, columns, t->stride(0)) : linear_rows{nullptr, 0};
+    }
+    // [K, N] with columns on end, or the transposed view of [N, K]
+    linear_rows weight(PyObject* o, int* K, int* N, int* rows_of_n) {
+        *rows_of_n = 0;
+        if (o == Py_None || !r.ok) return {nullptr, 0};
+        r.ok = r.ok && THPVariable_Check(o);
+        if (!r.ok) return {nullptr, 0};
+        const at::Tensor& t = THPVariable_Unpack(o);
+        r.ok = t.defined() && t.layout() == at::kStrided && t.is_cuda() && t.device().index() == r.device && t.dim() == 2 && t.numel() > 0 &&
+               t.size(0) <= INT_MAX && t.size(1) <= INT_MAX && (t.stride(0) == 1 || t.stride(1) == 1);
+        if (!r.ok) return {nullptr, 0};
+        *rows_of_n = t.stride(1) != 1;
+        return sized(t, K, N, t.stride(*rows_of_n));
+    }
+
+  private:
+    linear_rows sized(const at::Tensor& t, int* rows, int* columns, long long stride) {
+        if (!*rows) *rows = (int)t.size(0);
+        if (!*columns) *columns = (int)t.size(1);
+        if (t.scalar_type() != type || t.size(0) != *rows || t.size(1) != *columns) r.ok = false;
+        return {t.data_ptr(), stride};
+    }
+};
+
+// Index of an activation's name, as linear.ACTIVATIONS has them.
+int activation_of(PyObject* o, Reader& r) {
+    static const char* const names[] = {"none", "relu", "silu", "gelu", "gelu_tanh"};
+    if (o == Py_None) return 0;
+    if (PyUnicode_Check(o))
+        for (int i = 0; i < 5; ++i)
+            if (!PyUnicode_CompareWithASCIIString(o, names[i])) return i;
+    r.ok = false;
+    return 0;
+}
+
+// gemm_linear(x, w, out, bias, residual, pre, activation, workspace, stream), without a workspace of the caller's: one is left to Python.
+PyObject* linear(PyObject* const* args, Py_ssize_t nargs) {
+    if (nargs != 9 || !g_linear || args[7] != Py_None || args[2] == Py_None) return not_plain();
+    Reader r(args[0]);
+    LinearArgs a(r, args[0]);
+    int M = 0, N = 0, K = 0, rows_of_n;
+    const linear_rows x = a.matrix(args[0], &M, &K), w = a.weight(args[1], &K, &N, &rows_of_n), out = a.matrix(args[2], &M, &N),
+                      residual = a.matrix(args[4], &M, &N), pre = a.matrix(args[5], &M, &N);
+    const at::Tensor* bias = args[3] == Py_None ? nullptr : r.strided(args[3], 1);
+    const int act = activation_of(args[6], r), dt = a.dtype();
+    if (!r.ok || dt < 0 || !x.data || !w.data || (bias && (bias->size(0) != N || (bias->scalar_type() != a.type && bias->scalar_type() != at::kFloat))))
+        return not_plain();
+    void* stream;
+    if (!stream_of(args[8], THPVariable_Unpack(args[0]), &stream)) return not_plain();
+    const long long need = g_linear_workspace(M, N, K, rows_of_n);
+    if (need < 0) return PyLong_FromLong(need);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    {
+        Workspace own(stream, r.device, true);
+        void* ws = need ? own.take(need) : nullptr;
+        rc = g_linear(&x, &w, rows_of_n, bias ? bias->data_ptr() : nullptr, bias && bias->scalar_type() == at::kFloat, &residual, &pre, &out, act, M, N, K, dt,
+                      ws, ws ? need : 0, stream);
+    }
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+// gemm_linear_bwd(dy, x, w, pre, dx, dw, dbias, activation, workspace, stream), without a workspace of the caller's.
+PyObject* linear_bwd(PyObject* const* args, Py_ssize_t nargs) {
+    if (nargs != 10 || !g_linear_bwd || args[8] != Py_None || args[0] == Py_None) return not_plain();
+    Reader r(args[0]);
+    LinearArgs a(r, args[0]);
+    int M = 0, N = 0, K = 0, w_rows_of_n, dw_rows_of_n;
+    const int act = activation_of(args[7], r), dt = a.dtype();
+    const bool want_x = args[4] != Py_None, want_w = args[5] != Py_None;
+    const linear_rows dy = a.matrix(args[0], &M, &N), dx = a.matrix(args[4], &M, &K), dw = a.weight(args[5], &K, &N, &dw_rows_of_n),
+                      x = a.matrix(want_w ? args[1] : Py_None, &M, &K), w = a.weight(want_x ? args[2] : Py_None, &K, &N, &w_rows_of_n),
+                      pre = a.matrix(act ? args[3] : Py_None, &M, &N);
+    const at::Tensor* dbias = r.whole_or_none(args[6], 1, at::kFloat);
+    if (!r.ok || dt < 0 || (want_x && !w.data) || (want_w && !x.data) || (act && !pre.data) || (dbias && dbias->size(0) != N) || (!want_x && !want_w && !dbias))
+        return not_plain();
+    void* stream;
+    if (!stream_of(args[9], THPVariable_Unpack(args[0]), &stream)) return not_plain();
+    if (!K) K = 8;  // (dbias alone: no product)
+    const long long need = g_linear_bwd_workspace(M, N, K, w_rows_of_n, dw_rows_of_n, act, want_x, want_w, dbias != nullptr);
+    if (need < 0) return PyLong_FromLong(need);
+    long rc = kNotPlain;
+    float* const db = (float*)data(dbias);
+    Py_BEGIN_ALLOW_THREADS
+    {
+        Workspace own(stream, r.device, true);
+        void* ws = need ? own.take(need) : nullptr;
+        if (ws || !need) rc = g_linear_bwd(&dy, &x, &w, w_rows_of_n, &pre, &dx, &dw, dw_rows_of_n, db, act, M, N, K, dt, ws, need, stream);
+    }
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
 // memory_of_a_pool(address): whether torch's allocator has it in a pool other than the common one
 PyObject* memory_of_a_pool(PyObject* const* args, Py_ssize_t nargs) {
     if (nargs != 1) return not_plain();
@@ -439,6 +552,15 @@ PyObject* bind_cached(PyObject*, PyObject* args) {
     g_kv4_append = (decltype(g_kv4_append))f[0], g_kv4_read = (decltype(g_kv4_read))f[1], g_kv4_attn = (decltype(g_kv4_attn))f[2];
     g_kv4_attn_workspace = (decltype(g_kv4_attn_workspace))f[3], g_rope = (decltype(g_rope))f[4], g_rope_bwd = (decltype(g_rope_bwd))f[5];
     g_rope_bwd_workspace = (decltype(g_rope_bwd_workspace))f[6];
+    Py_RETURN_NONE;
+}
+
+// bind_linear(addresses of gemm_linear, gemm_linear_workspace, gemm_linear_bwd and gemm_linear_bwd_workspace)
+PyObject* bind_linear(PyObject*, PyObject* args) {
+    unsigned long long f[4];
+    if (!PyArg_ParseTuple(args, "KKKK", &f[0], &f[1], &f[2], &f[3])) return nullptr;
+    g_linear = (decltype(g_linear))f[0], g_linear_workspace = (decltype(g_linear_workspace))f[1];
+    g_linear_bwd = (decltype(g_linear_bwd))f[2], g_linear_bwd_workspace = (decltype(g_linear_bwd_workspace))f[3];
     Py_RETURN_NONE;
 }
 
@@ -459,8 +581,11 @@ PyMethodDef methods[] = {{"attn_fwd", (PyCFunction)(void (*)(void))guarded<attn_
                          {"kv4_attn", (PyCFunction)(void (*)(void))guarded<cached_attn>, METH_FASTCALL, "0, a library error, or NOT_PLAIN"},
                          {"qk_norm_rope", (PyCFunction)(void (*)(void))guarded<norm_rope>, METH_FASTCALL, "0, a library error, or NOT_PLAIN"},
                          {"qk_norm_rope_bwd", (PyCFunction)(void (*)(void))guarded<norm_rope_bwd>, METH_FASTCALL, "0, a library error, or NOT_PLAIN"},
+                         {"gemm_linear", (PyCFunction)(void (*)(void))guarded<linear>, METH_FASTCALL, "0, a library error, or NOT_PLAIN"},
+                         {"gemm_linear_bwd", (PyCFunction)(void (*)(void))guarded<linear_bwd>, METH_FASTCALL, "0, a library error, or NOT_PLAIN"},
                          {"memory_of_a_pool", (PyCFunction)(void (*)(void))guarded<memory_of_a_pool>, METH_FASTCALL, "whether an address is a private pool's"},
                          {"bind_cached", bind_cached, METH_VARARGS, "addresses of the library's entry points"},
+                         {"bind_linear", bind_linear, METH_VARARGS, "addresses of the library's entry points"},
                          {"bind", bind, METH_VARARGS, "addresses of the library's entry points"},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
