@@ -60,6 +60,20 @@ int qk_norm_rope_bwd(const qk_heads* dq_out, const qk_heads* dk_out, const qk_he
                      float* dk_weight, const float* cos, const float* sin, const int* positions, int rows, float eps, int interleaved,
                      int B, int N, int H, int Hkv, int d, int dtype, void* workspace, long long workspace_bytes, void* stream);
 
+/* The same with a rotation by positions on several axes (time, height and width of a video's patches, say): pair p turns by the row of cos and sin that the
+ * token's position on the pair's own axis names.
+ *  positions    : device, int32 [B, N, axes], axes 1 .. 4; one outside 0 .. rows-1 makes the outputs (backward: gradients) of that axis's pairs NaN (backward
+ *                 with a weight: of all pairs of the token).
+ *  axis_of_pair : HOST, d/2 values, read before the call returns: the axis of each pair, 0 .. axes-1, or QK_NO_AXIS for a pair that is not turned. */
+#define QK_NO_AXIS 255
+int qk_norm_rope_axes(const qk_heads* q, const qk_heads* k, const qk_heads* q_out, const qk_heads* k_out, const void* q_weight,
+                      const void* k_weight, int weight_f32, const float* cos, const float* sin, const int* positions, int rows, int axes,
+                      const unsigned char* axis_of_pair, float eps, int interleaved, int B, int N, int H, int Hkv, int d, int dtype, void* stream);
+int qk_norm_rope_axes_bwd(const qk_heads* dq_out, const qk_heads* dk_out, const qk_heads* q, const qk_heads* k, const qk_heads* dq,
+                          const qk_heads* dk, const void* q_weight, const void* k_weight, int weight_f32, float* dq_weight, float* dk_weight,
+                          const float* cos, const float* sin, const int* positions, int rows, int axes, const unsigned char* axis_of_pair, float eps,
+                          int interleaved, int B, int N, int H, int Hkv, int d, int dtype, void* workspace, long long workspace_bytes, void* stream);
+
 /* Bytes for B sequences of N tokens; negative: the error that the call would give. */
 long long qk_norm_rope_bwd_workspace(int B, int N, int H, int Hkv, int d);
 

@@ -25,7 +25,8 @@ LINEAR_PARTS = 6        # layouts and types of the linear layers' products (csrc
 
 # (object, source, extra flags)
 UNITS = [("attn_fwd.o", "attn_fwd.hip", []), ("gemm_lrelu.o", "gemm_lrelu.hip", []), ("kv4_cache.o", "kv4_cache.hip", []),
-         ("kv4_attn.o", "kv4_attn.hip", []), ("qk_rope.o", "qk_rope.hip", []), ("linear.o", "linear.hip", [])] + \
+         ("kv4_attn.o", "kv4_attn.hip", []), ("qk_rope.o", "qk_rope.hip", []), ("linear.o", "linear.hip", []),
+         ("residual_norm.o", "residual_norm.hip", [])] + \
         [(f"linear_kernels_{p}.o", "linear_kernels.hip", [f"-DLINEAR_PART={p}"]) for p in range(LINEAR_PARTS)] + \
         [(f"attn_kernels_{p}.o", "attn_kernels.hip", [f"-DATTN_PART={p}"]) for p in range(ATTN_PARTS)]
 

@@ -20,6 +20,7 @@
 #include "../../include/kv4.h"
 #include "../../include/linear.h"
 #include "../../include/qk_rope.h"
+#include "../../include/residual_norm.h"
 
 namespace {
 
@@ -39,10 +40,15 @@ decltype(&kv4_attn_workspace) g_kv4_attn_workspace = nullptr;
 decltype(&qk_norm_rope) g_rope = nullptr;
 decltype(&qk_norm_rope_bwd) g_rope_bwd = nullptr;
 decltype(&qk_norm_rope_bwd_workspace) g_rope_bwd_workspace = nullptr;
+decltype(&qk_norm_rope_axes) g_rope_axes = nullptr;
+decltype(&qk_norm_rope_axes_bwd) g_rope_axes_bwd = nullptr;
 decltype(&gemm_linear) g_linear = nullptr;
 decltype(&gemm_linear_workspace) g_linear_workspace = nullptr;
 decltype(&gemm_linear_bwd) g_linear_bwd = nullptr;
 decltype(&gemm_linear_bwd_workspace) g_linear_bwd_workspace = nullptr;
+decltype(&residual_norm) g_norm = nullptr;
+decltype(&residual_norm_bwd) g_norm_bwd = nullptr;
+decltype(&residual_norm_bwd_workspace) g_norm_bwd_workspace = nullptr;
 
 // Whether torch's allocator has an address in a pool of its own: one that it opened for a graph that it records (or its user for tensors).  It looks
 // through all segments, which a recording can wait for.
@@ -341,6 +347,8 @@ struct RopeArgs {
     const at::Tensor* like = nullptr;
     int heads[2] = {0, 0}, dt = -1, B = 0, N = 0, d = 0, f32 = 0;
     const at::Tensor *cos = nullptr, *sin = nullptr, *positions = nullptr, *w[2] = {nullptr, nullptr};
+    int axes = 0;  // 0: one position a token
+    const unsigned char* axis_of_pair = nullptr;
 
     // A tensor of heads (z: of queries or keys) of one type and the sizes of those before it; None where `heads` has none.
     bool heads_of(Reader& r, PyObject* o, int z, qk_heads* h) {
@@ -354,10 +362,18 @@ struct RopeArgs {
         *h = {t->data_ptr(), stride(t, 0), stride(t, 1), stride(t, 2)};
         return true;
     }
-    bool others(Reader& r, PyObject* const* a) {  // cos, sin, positions, q_weight, k_weight
+    // cos, sin, positions, q_weight, k_weight; by axes: cos, sin, positions, axes, q_weight, k_weight
+    bool others(Reader& r, PyObject* const* a, bool by_axes) {
         if (!tables(r, a[0], a[1], d, &cos, &sin)) return false;
-        positions = r.whole(a[2], 2, at::kInt);
+        positions = r.whole(a[2], by_axes ? 3 : 2, at::kInt);
         if (!r.ok || positions->size(0) != B || positions->size(1) != N) return false;
+        if (by_axes) {
+            if (!PyBytes_CheckExact(a[3]) || PyBytes_GET_SIZE(a[3]) != d / 2 || positions->size(2) > 4) return false;
+            axes = (int)positions->size(2), axis_of_pair = (const unsigned char*)PyBytes_AS_STRING(a[3]);  // (the caller holds the object)
+            for (int p = 0; p < d / 2; ++p)
+                if (axis_of_pair[p] >= axes && axis_of_pair[p] != QK_NO_AXIS) return false;
+            ++a;
+        }
         for (int z = 0; z < 2; ++z) {
             if (a[3 + z] == Py_None) continue;
             w[z] = r.strided(a[3 + z], 1);
@@ -370,9 +386,10 @@ struct RopeArgs {
     }
 };
 
-// qk_norm_rope(q, k, q_out, k_out, cos, sin, positions, q_weight, k_weight, eps, interleaved, stream)
+// qk_norm_rope(q, k, q_out, k_out, cos, sin, positions, q_weight, k_weight, eps, interleaved, stream), by axes with `axes` behind positions
+template <bool AXES>
 PyObject* norm_rope(PyObject* const* args, Py_ssize_t nargs) {
-    if (nargs != 12 || !g_rope) return not_plain();
+    if (nargs != 12 + AXES || (AXES ? !g_rope_axes : !g_rope)) return not_plain();
     Reader r(args[4]);
     RopeArgs a;
     qk_heads h[4];
@@ -380,41 +397,49 @@ PyObject* norm_rope(PyObject* const* args, Py_ssize_t nargs) {
         if (!a.heads_of(r, args[i], i % 2, &h[i])) return not_plain();
     for (int z = 0; z < 2; ++z)
         if (!h[z].data != !h[2 + z].data) return not_plain();
-    if (!a.like || !a.others(r, args + 4)) return not_plain();
+    if (!a.like || !a.others(r, args + 4, AXES)) return not_plain();
+    args += AXES;
     const double eps = r.number(args[9]);
     const bool pairs = r.truth(args[10]);
     void* stream;
     if (!r.ok || !stream_of(args[11], *a.like, &stream)) return not_plain();
     int rc;
     Py_BEGIN_ALLOW_THREADS
-    rc = g_rope(&h[0], &h[1], &h[2], &h[3], data(a.w[0]), data(a.w[1]), a.f32, (const float*)data(a.cos), (const float*)data(a.sin),
-                (const int*)data(a.positions), (int)a.cos->size(0), (float)eps, pairs, a.B, a.N, a.heads[0], a.heads[1], a.d, a.dt, stream);
+    if (AXES)
+        rc = g_rope_axes(&h[0], &h[1], &h[2], &h[3], data(a.w[0]), data(a.w[1]), a.f32, (const float*)data(a.cos), (const float*)data(a.sin),
+                         (const int*)data(a.positions), (int)a.cos->size(0), a.axes, a.axis_of_pair, (float)eps, pairs, a.B, a.N, a.heads[0], a.heads[1],
+                         a.d, a.dt, stream);
+    else
+        rc = g_rope(&h[0], &h[1], &h[2], &h[3], data(a.w[0]), data(a.w[1]), a.f32, (const float*)data(a.cos), (const float*)data(a.sin),
+                    (const int*)data(a.positions), (int)a.cos->size(0), (float)eps, pairs, a.B, a.N, a.heads[0], a.heads[1], a.d, a.dt, stream);
     Py_END_ALLOW_THREADS
     return PyLong_FromLong(rc);
 }
 
-// qk_norm_rope_bwd(dq_out, dk_out, q, k, dq, dk, cos, sin, positions, q_weight, k_weight, dq_weight, dk_weight, eps, interleaved, workspace, stream),
-// without a workspace of the caller's: one is left to Python.
+// qk_norm_rope_bwd(dq_out, dk_out, q, k, dq, dk, cos, sin, positions, q_weight, k_weight, dq_weight, dk_weight, eps, interleaved, workspace, stream), by axes
+// with `axes` behind positions, without a workspace of the caller's: one is left to Python.
+template <bool AXES>
 PyObject* norm_rope_bwd(PyObject* const* args, Py_ssize_t nargs) {
-    if (nargs != 17 || !g_rope_bwd || args[15] != Py_None) return not_plain();
+    if (nargs != 17 + AXES || (AXES ? !g_rope_axes_bwd : !g_rope_bwd) || args[15 + AXES] != Py_None) return not_plain();
+    PyObject* const* const more = args + AXES;  // from the weights on
     Reader r(args[6]);
     RopeArgs a;
     qk_heads h[6];
     for (int i : {0, 1, 4, 5})
         if (!a.heads_of(r, args[i], i % 2, &h[i])) return not_plain();
     for (int z = 0; z < 2; ++z) {
-        if (!h[z].data != !h[4 + z].data || (args[9 + z] != Py_None && !h[z].data) || (args[9 + z] == Py_None) != (args[11 + z] == Py_None)) return not_plain();
+        if (!h[z].data != !h[4 + z].data || (more[9 + z] != Py_None && !h[z].data) || (more[9 + z] == Py_None) != (more[11 + z] == Py_None)) return not_plain();
         h[2 + z] = {nullptr, 0, 0, 0};
-        if (args[9 + z] != Py_None && (args[2 + z] == Py_None || !a.heads_of(r, args[2 + z], z, &h[2 + z]))) return not_plain();
+        if (more[9 + z] != Py_None && (args[2 + z] == Py_None || !a.heads_of(r, args[2 + z], z, &h[2 + z]))) return not_plain();
     }
-    if (!a.like || !a.others(r, args + 6)) return not_plain();
-    const at::Tensor* dw[2] = {r.whole_or_none(args[11], 1, at::kFloat), r.whole_or_none(args[12], 1, at::kFloat)};
+    if (!a.like || !a.others(r, args + 6, AXES)) return not_plain();
+    const at::Tensor* dw[2] = {r.whole_or_none(more[11], 1, at::kFloat), r.whole_or_none(more[12], 1, at::kFloat)};
     for (int z = 0; z < 2; ++z)
         if (r.ok && dw[z] && dw[z]->size(0) != a.d) return not_plain();
-    const double eps = r.number(args[13]);
-    const bool pairs = r.truth(args[14]);
+    const double eps = r.number(more[13]);
+    const bool pairs = r.truth(more[14]);
     void* stream;
-    if (!r.ok || !stream_of(args[16], *a.like, &stream)) return not_plain();
+    if (!r.ok || !stream_of(more[16], *a.like, &stream)) return not_plain();
     const long long need = a.w[0] || a.w[1] ? g_rope_bwd_workspace(a.B, a.N, a.heads[0], a.heads[1], a.d) : 0;
     if (need < 0) return PyLong_FromLong(need);
     long rc = kNotPlain;
@@ -422,7 +447,11 @@ PyObject* norm_rope_bwd(PyObject* const* args, Py_ssize_t nargs) {
     {
         Workspace own(stream, r.device, true);
         void* ws = need ? own.take(need) : nullptr;
-        if (ws || !need)
+        if ((ws || !need) && AXES)
+            rc = g_rope_axes_bwd(&h[0], &h[1], &h[2], &h[3], &h[4], &h[5], data(a.w[0]), data(a.w[1]), a.f32, (float*)data(dw[0]), (float*)data(dw[1]),
+                                 (const float*)data(a.cos), (const float*)data(a.sin), (const int*)data(a.positions), (int)a.cos->size(0), a.axes,
+                                 a.axis_of_pair, (float)eps, pairs, a.B, a.N, a.heads[0], a.heads[1], a.d, a.dt, ws, need, stream);
+        else if (ws || !need)
             rc = g_rope_bwd(&h[0], &h[1], &h[2], &h[3], &h[4], &h[5], data(a.w[0]), data(a.w[1]), a.f32, (float*)data(dw[0]), (float*)data(dw[1]),
                             (const float*)data(a.cos), (const float*)data(a.sin), (const int*)data(a.positions), (int)a.cos->size(0), (float)eps, pairs,
                             a.B, a.N, a.heads[0], a.heads[1], a.d, a.dt, ws, need, stream);
@@ -539,6 +568,100 @@ PyObject* linear_bwd(PyObject* const* args, Py_ssize_t nargs) {
     return PyLong_FromLong(rc);
 }
 
+// Norms with the residual stream: tensors [B, N, C] of one type and size.
+
+struct NormArgs {
+    const at::Tensor* like = nullptr;
+    int B = 0, N = 0, C = 0, dt = -1;
+    norm_vectors v = {};
+
+    norm_tokens tokens(Reader& r, PyObject* o) {
+        if (o == Py_None) return {nullptr, 0, 0};
+        const at::Tensor* t = r.strided(o, 3);
+        if (!t) return {nullptr, 0, 0};
+        if (!like) like = t, dt = dtype_code(*t), B = (int)t->size(0), N = (int)t->size(1), C = (int)t->size(2);
+        if (dt < 0 || t->scalar_type() != like->scalar_type() || t->sizes() != like->sizes()) r.ok = false;
+        return {t->data_ptr(), stride(t, 0), stride(t, 1)};
+    }
+    const void* vector(Reader& r, PyObject* o, int* f32, bool first) {
+        if (o == Py_None || !r.ok) return nullptr;
+        const at::Tensor* t = r.strided(o, 1);
+        if (!t) return nullptr;
+        const bool wide = t->scalar_type() == at::kFloat;
+        if (t->size(0) != C || (!wide && t->scalar_type() != like->scalar_type()) || (!first && *f32 != wide)) r.ok = false;
+        *f32 = wide;
+        return t->data_ptr();
+    }
+    // gate, post_weight, pre_weight, then (elsewhere) alpha, eps
+    bool vectors(Reader& r, PyObject* const* a, PyObject* alpha, PyObject* eps) {
+        if (!r.ok || !like) return false;
+        if (a[0] != Py_None && THPVariable_Check(a[0]) && THPVariable_Unpack(a[0]).defined() && THPVariable_Unpack(a[0]).dim() == 2) {
+            const at::Tensor* t = r.strided(a[0], 2);
+            if (!t) return false;
+            v.gate_f32 = t->scalar_type() == at::kFloat;
+            if (t->size(0) != B || t->size(1) != C || (!v.gate_f32 && t->scalar_type() != like->scalar_type()) || (B > 1 && t->stride(0) < C)) return false;
+            v.gate = t->data_ptr(), v.gate_stride = B > 1 ? t->stride(0) : C;
+        } else {
+            v.gate = vector(r, a[0], &v.gate_f32, true);
+        }
+        v.post_weight = vector(r, a[1], &v.weight_f32, true);
+        v.pre_weight = vector(r, a[2], &v.weight_f32, a[1] == Py_None);
+        v.alpha = (float)r.number(alpha), v.eps = (float)r.number(eps);
+        return r.ok;
+    }
+};
+
+// residual_norm(x, h, y, z, gate, post_weight, pre_weight, alpha, eps, stream)
+PyObject* norm(PyObject* const* args, Py_ssize_t nargs) {
+    if (nargs != 10 || !g_norm || args[0] == Py_None) return not_plain();
+    Reader r(args[0]);
+    NormArgs a;
+    const norm_tokens x = a.tokens(r, args[0]), h = a.tokens(r, args[1]), y = a.tokens(r, args[2]), z = a.tokens(r, args[3]);
+    void* stream;
+    if (!a.vectors(r, args + 4, args[7], args[8]) || (!y.data && !z.data) || (z.data != nullptr) != (a.v.pre_weight != nullptr) ||
+        (!h.data && (y.data || a.v.gate || a.v.post_weight || a.v.alpha != 1.f)) || !stream_of(args[9], *a.like, &stream))
+        return not_plain();
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = g_norm(&x, &h, &y, &z, &a.v, a.B, a.N, a.C, a.dt, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+// residual_norm_bwd(dy, dz, y, h, dx, dh, gate, post_weight, pre_weight, dgate, dpost_weight, dpre_weight, alpha, eps, workspace, stream), without a
+// workspace of the caller's.
+PyObject* norm_bwd(PyObject* const* args, Py_ssize_t nargs) {
+    if (nargs != 16 || !g_norm_bwd || args[14] != Py_None) return not_plain();
+    Reader r(args[0] != Py_None ? args[0] : args[1]);
+    NormArgs a;
+    const bool need_y = args[1] != Py_None, need_h = args[6] != Py_None || args[7] != Py_None;
+    const norm_tokens dy = a.tokens(r, args[0]), dz = a.tokens(r, args[1]), y = a.tokens(r, need_y ? args[2] : Py_None),
+                      h = a.tokens(r, need_h ? args[3] : Py_None), dx = a.tokens(r, args[4]), dh = a.tokens(r, args[5]);
+    if (!a.vectors(r, args + 6, args[12], args[13]) || (need_y && !y.data) || (need_h && !h.data) || (!dx.data && !dh.data) ||
+        (dz.data != nullptr) != (a.v.pre_weight != nullptr))
+        return not_plain();
+    float* grads[3];
+    for (int i = 0; i < 3; ++i) {  // of the shape of their vectors
+        const bool rows = i == 0 && a.v.gate && a.v.gate_stride;
+        const at::Tensor* t = r.whole_or_none(args[9 + i], rows ? 2 : 1, at::kFloat);
+        if (!r.ok || (t && (args[6 + i] == Py_None || t->size(rows) != a.C || (rows && t->size(0) != a.B)))) return not_plain();
+        grads[i] = (float*)data(t);
+    }
+    void* stream;
+    if (!stream_of(args[15], *a.like, &stream)) return not_plain();
+    const long long need = grads[0] || grads[1] || grads[2] ? g_norm_bwd_workspace(a.B, a.N, a.C, a.v.gate && a.v.gate_stride) : 0;
+    if (need < 0) return PyLong_FromLong(need);
+    long rc = kNotPlain;
+    Py_BEGIN_ALLOW_THREADS
+    {
+        Workspace own(stream, r.device, true);
+        void* ws = need ? own.take(need) : nullptr;
+        if (ws || !need) rc = g_norm_bwd(&dy, &dz, &y, &h, &dx, &dh, &a.v, grads[0], grads[1], grads[2], a.B, a.N, a.C, a.dt, ws, need, stream);
+    }
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
 // memory_of_a_pool(address): whether torch's allocator has it in a pool other than the common one
 PyObject* memory_of_a_pool(PyObject* const* args, Py_ssize_t nargs) {
     if (nargs != 1) return not_plain();
@@ -555,12 +678,15 @@ PyObject* bind_cached(PyObject*, PyObject* args) {
     Py_RETURN_NONE;
 }
 
-// bind_linear(addresses of gemm_linear, gemm_linear_workspace, gemm_linear_bwd and gemm_linear_bwd_workspace)
-PyObject* bind_linear(PyObject*, PyObject* args) {
-    unsigned long long f[4];
-    if (!PyArg_ParseTuple(args, "KKKK", &f[0], &f[1], &f[2], &f[3])) return nullptr;
+// bind_block(addresses of gemm_linear, gemm_linear_workspace, gemm_linear_bwd, gemm_linear_bwd_workspace, residual_norm, residual_norm_bwd,
+// residual_norm_bwd_workspace, qk_norm_rope_axes and qk_norm_rope_axes_bwd)
+PyObject* bind_block(PyObject*, PyObject* args) {
+    unsigned long long f[9];
+    if (!PyArg_ParseTuple(args, "KKKKKKKKK", &f[0], &f[1], &f[2], &f[3], &f[4], &f[5], &f[6], &f[7], &f[8])) return nullptr;
+    g_rope_axes = (decltype(g_rope_axes))f[7], g_rope_axes_bwd = (decltype(g_rope_axes_bwd))f[8];
     g_linear = (decltype(g_linear))f[0], g_linear_workspace = (decltype(g_linear_workspace))f[1];
     g_linear_bwd = (decltype(g_linear_bwd))f[2], g_linear_bwd_workspace = (decltype(g_linear_bwd_workspace))f[3];
+    g_norm = (decltype(g_norm))f[4], g_norm_bwd = (decltype(g_norm_bwd))f[5], g_norm_bwd_workspace = (decltype(g_norm_bwd_workspace))f[6];
     Py_RETURN_NONE;
 }
 
@@ -579,13 +705,17 @@ PyMethodDef methods[] = {{"attn_fwd", (PyCFunction)(void (*)(void))guarded<attn_
                          {"kv4_append", (PyCFunction)(void (*)(void))guarded<append>, METH_FASTCALL, "0, a library error, or NOT_PLAIN"},
                          {"kv4_read", (PyCFunction)(void (*)(void))guarded<read>, METH_FASTCALL, "0, a library error, or NOT_PLAIN"},
                          {"kv4_attn", (PyCFunction)(void (*)(void))guarded<cached_attn>, METH_FASTCALL, "0, a library error, or NOT_PLAIN"},
-                         {"qk_norm_rope", (PyCFunction)(void (*)(void))guarded<norm_rope>, METH_FASTCALL, "0, a library error, or NOT_PLAIN"},
-                         {"qk_norm_rope_bwd", (PyCFunction)(void (*)(void))guarded<norm_rope_bwd>, METH_FASTCALL, "0, a library error, or NOT_PLAIN"},
+                         {"qk_norm_rope", (PyCFunction)(void (*)(void))guarded<norm_rope<false>>, METH_FASTCALL, "0, a library error, or NOT_PLAIN"},
+                         {"qk_norm_rope_bwd", (PyCFunction)(void (*)(void))guarded<norm_rope_bwd<false>>, METH_FASTCALL, "0, a library error, or NOT_PLAIN"},
                          {"gemm_linear", (PyCFunction)(void (*)(void))guarded<linear>, METH_FASTCALL, "0, a library error, or NOT_PLAIN"},
                          {"gemm_linear_bwd", (PyCFunction)(void (*)(void))guarded<linear_bwd>, METH_FASTCALL, "0, a library error, or NOT_PLAIN"},
+                         {"residual_norm", (PyCFunction)(void (*)(void))guarded<norm>, METH_FASTCALL, "0, a library error, or NOT_PLAIN"},
+                         {"residual_norm_bwd", (PyCFunction)(void (*)(void))guarded<norm_bwd>, METH_FASTCALL, "0, a library error, or NOT_PLAIN"},
+                         {"qk_norm_rope_axes", (PyCFunction)(void (*)(void))guarded<norm_rope<true>>, METH_FASTCALL, "0, a library error, or NOT_PLAIN"},
+                         {"qk_norm_rope_axes_bwd", (PyCFunction)(void (*)(void))guarded<norm_rope_bwd<true>>, METH_FASTCALL, "0, a library error, or NOT_PLAIN"},
                          {"memory_of_a_pool", (PyCFunction)(void (*)(void))guarded<memory_of_a_pool>, METH_FASTCALL, "whether an address is a private pool's"},
                          {"bind_cached", bind_cached, METH_VARARGS, "addresses of the library's entry points"},
-                         {"bind_linear", bind_linear, METH_VARARGS, "addresses of the library's entry points"},
+                         {"bind_block", bind_block, METH_VARARGS, "addresses of the library's entry points"},
                          {"bind", bind, METH_VARARGS, "addresses of the library's entry points"},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -9,6 +9,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "../../include/qk_rope.h"
 #include "kv4_format.h"
 
@@ -36,6 +38,14 @@ struct Args {
     float eps;
 };
 
+// By several axes: a token has a position on each, and lane l's 8 pairs turn by the axes in the nibbles of axis[l], kNoAxis: not at all.
+struct AxesArgs : Args {
+    int axes;
+    unsigned axis[8];
+};
+constexpr unsigned kNoAxis = 15;
+constexpr int kMostAxes = 4;
+
 constexpr int kTokens = 8;
 
 template <int D, bool BF>
@@ -61,8 +71,33 @@ __device__ __forceinline__ float vector_sum(float x) {
     return x;
 }
 
-template <int D, bool BF, bool BACK, bool PAIRS>
-__global__ __launch_bounds__(256, 4) void rope_kernel(Args a) {
+// The cosines and sines of a lane's 8 pairs by several axes, `mine` its word of AxesArgs::axis.  Axes mostly begin and end between lanes, and then a lane
+// reads one row of the tables; one whose pairs have several axes reads a row for each and takes its pairs from it.
+template <int D>
+__device__ __forceinline__ void angles_by_axes(const float* cos, const float* sin, const int* positions, int rows, int axes, unsigned mine, int l, float* c, float* s) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c[i] = 1, s[i] = 0;
+    for (int axis = 0; axis < axes; ++axis) {
+        unsigned other = mine ^ axis * 0x11111111u;  // nibbles of 0: this axis's pairs
+        other = (other | other >> 1 | other >> 2 | other >> 3) & 0x11111111u;
+        if (other == 0x11111111u) continue;
+        const int at = positions[axis];
+        float x[8], y[8];
+        if ((unsigned)at < (unsigned)rows) {
+            load8f(cos + (long long)at * (D / 2) + 8 * l, x);
+            load8f(sin + (long long)at * (D / 2) + 8 * l, y);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = y[i] = __uint_as_float(0x7fc00000u);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (!(other >> 4 * i & 1)) c[i] = x[i], s[i] = y[i];
+    }
+}
+
+template <int D, bool BF, bool BACK, bool PAIRS, class ARGS>
+__global__ __launch_bounds__(256, 4) void rope_kernel(ARGS a) {
     constexpr int L = D / 16, SLOTS = 256 / L, PHASES = SLOTS / kTokens, PARTS = 256 / D;
     __shared__ float sums[BACK ? SLOTS * (D + 4) : 1], parts[BACK ? 256 : 1];
     const int l = threadIdx.x % L, slot = threadIdx.x / L, phase = slot / kTokens;
@@ -89,12 +124,16 @@ __global__ __launch_bounds__(256, 4) void rope_kernel(Args a) {
             if (token >= a.tokens) break;  // no later tile has one for this lane; the lanes of a vector leave together
             const long long b = token / a.N, n = token % a.N;
             float c[8], s[8];
-            const int at = a.positions[token];
-            if ((unsigned)at < (unsigned)a.rows) {
-                load8f(a.cos + (long long)at * (D / 2) + 8 * l, c);
-                load8f(a.sin + (long long)at * (D / 2) + 8 * l, s);
+            if constexpr (std::is_same_v<ARGS, AxesArgs>) {
+                angles_by_axes<D>(a.cos, a.sin, a.positions + token * a.axes, a.rows, a.axes, a.axis[l], l, c, s);
             } else {
-                for (int i = 0; i < 8; ++i) c[i] = s[i] = __uint_as_float(0x7fc00000u);
+                const int at = a.positions[token];
+                if ((unsigned)at < (unsigned)a.rows) {
+                    load8f(a.cos + (long long)at * (D / 2) + 8 * l, c);
+                    load8f(a.sin + (long long)at * (D / 2) + 8 * l, s);
+                } else {
+                    for (int i = 0; i < 8; ++i) c[i] = s[i] = __uint_as_float(0x7fc00000u);
+                }
             }
             const uint16_t* x = T.x + b * T.xs[0] + n * T.xs[1];
             const uint16_t* dy = T.dy + b * T.dys[0] + n * T.dys[1];
@@ -239,31 +278,44 @@ bool meets(const qk_heads* out, const qk_heads* other, bool own, int B, int N, i
 
 void strides(const qk_heads* t, long long* s) { s[0] = t->batch_stride, s[1] = t->token_stride, s[2] = t->head_stride; }
 
-template <bool BACK>
+template <bool BACK, class ARGS>
 const void* kernel(int d, int dtype, int pairs) {
     if (d == 128) {
-        if (dtype) return pairs ? (const void*)rope_kernel<128, true, BACK, true> : (const void*)rope_kernel<128, true, BACK, false>;
-        return pairs ? (const void*)rope_kernel<128, false, BACK, true> : (const void*)rope_kernel<128, false, BACK, false>;
+        if (dtype) return pairs ? (const void*)rope_kernel<128, true, BACK, true, ARGS> : (const void*)rope_kernel<128, true, BACK, false, ARGS>;
+        return pairs ? (const void*)rope_kernel<128, false, BACK, true, ARGS> : (const void*)rope_kernel<128, false, BACK, false, ARGS>;
     }
-    if (dtype) return pairs ? (const void*)rope_kernel<64, true, BACK, true> : (const void*)rope_kernel<64, true, BACK, false>;
-    return pairs ? (const void*)rope_kernel<64, false, BACK, true> : (const void*)rope_kernel<64, false, BACK, false>;
+    if (dtype) return pairs ? (const void*)rope_kernel<64, true, BACK, true, ARGS> : (const void*)rope_kernel<64, true, BACK, false, ARGS>;
+    return pairs ? (const void*)rope_kernel<64, false, BACK, true, ARGS> : (const void*)rope_kernel<64, false, BACK, false, ARGS>;
 }
 
-}  // namespace qk
+// The axes of a call, null for the calls of one position a token.
+struct Axes {
+    int count;
+    const unsigned char* of_pair;
+};
 
-extern "C" {
+bool fill(AxesArgs* to, const Axes& axes, int d) {
+    if (axes.count < 1 || axes.count > kMostAxes || !axes.of_pair) return false;
+    to->axes = axes.count;
+    for (int p = 0; p < d / 2; ++p) {
+        const unsigned axis = axes.of_pair[p];
+        if (axis != QK_NO_AXIS && axis >= (unsigned)axes.count) return false;
+        to->axis[p / 8] |= (axis == QK_NO_AXIS ? kNoAxis : axis) << 4 * (p % 8);
+    }
+    return true;
+}
 
-int qk_norm_rope(const qk_heads* q, const qk_heads* k, const qk_heads* q_out, const qk_heads* k_out, const void* q_weight,
-                 const void* k_weight, int weight_f32, const float* cos, const float* sin, const int* positions, int rows, float eps,
-                 int interleaved, int B, int N, int H, int Hkv, int d, int dtype, void* stream) {
-    using namespace qk;
+int forward(const qk_heads* q, const qk_heads* k, const qk_heads* q_out, const qk_heads* k_out, const void* q_weight, const void* k_weight,
+            int weight_f32, const float* cos, const float* sin, const int* positions, int rows, const Axes* axes, float eps, int interleaved, int B,
+            int N, int H, int Hkv, int d, int dtype, void* stream) {
     if (given(q) != given(q_out) || given(k) != given(k_out)) return QK_EINVAL;
     if (!given(q)) H = 0;
     if (!given(k)) Hkv = 0;
     if (!cos || !sin || !positions || rows < 1 || (dtype != QK_F16 && dtype != QK_BF16) || !(eps >= 0) || !isfinite(eps)) return QK_EINVAL;
     if ((uintptr_t)cos % 16 || (uintptr_t)sin % 16 || (uintptr_t)positions % 4 || (uintptr_t)q_weight % 16 || (uintptr_t)k_weight % 16) return QK_EINVAL;
     if (const int rc = check(B, N, H, Hkv, d)) return rc;
-    Args a = {};
+    AxesArgs a = {};
+    if (axes && !fill(&a, *axes, d)) return QK_EINVAL;
     const qk_heads* in[2] = {q, k};
     const qk_heads* out[2] = {q_out, k_out};
     const void* w[2] = {q_weight, k_weight};
@@ -281,26 +333,19 @@ int qk_norm_rope(const qk_heads* q, const qk_heads* k, const qk_heads* q_out, co
     const Grid g = grid_of((long long)B * N, H + Hkv, d, false);
     a.cos = cos, a.sin = sin, a.positions = positions, a.tokens = (long long)B * N, a.N = N, a.rows = rows, a.interleaved = interleaved;
     a.weight_f32 = weight_f32, a.head_step = g.head_step, a.blocks_y = g.y, a.eps = eps;
-    void* list[] = {&a};
-    if (hipLaunchKernel(kernel<false>(d, dtype, interleaved), dim3((unsigned)g.x * g.y), dim3(256), list, 0, (hipStream_t)stream) != hipSuccess) {
+    void* list[] = {axes ? (void*)&a : (void*)static_cast<Args*>(&a)};
+    const void* const fn = axes ? kernel<false, AxesArgs>(d, dtype, interleaved) : kernel<false, Args>(d, dtype, interleaved);
+    if (hipLaunchKernel(fn, dim3((unsigned)g.x * g.y), dim3(256), list, 0, (hipStream_t)stream) != hipSuccess) {
         (void)hipGetLastError();
         return QK_ELAUNCH;
     }
     return QK_OK;
 }
 
-long long qk_norm_rope_bwd_workspace(int B, int N, int H, int Hkv, int d) {
-    using namespace qk;
-    if (const int rc = check(B, N, H, Hkv, d)) return rc;
-    const Grid g = grid_of((long long)B * N, H + Hkv, d, true);
-    return (long long)g.x * g.y * 2 * d * 4;
-}
-
-int qk_norm_rope_bwd(const qk_heads* dq_out, const qk_heads* dk_out, const qk_heads* q, const qk_heads* k, const qk_heads* dq,
-                     const qk_heads* dk, const void* q_weight, const void* k_weight, int weight_f32, float* dq_weight,
-                     float* dk_weight, const float* cos, const float* sin, const int* positions, int rows, float eps, int interleaved,
-                     int B, int N, int H, int Hkv, int d, int dtype, void* workspace, long long workspace_bytes, void* stream) {
-    using namespace qk;
+int backward(const qk_heads* dq_out, const qk_heads* dk_out, const qk_heads* q, const qk_heads* k, const qk_heads* dq, const qk_heads* dk,
+             const void* q_weight, const void* k_weight, int weight_f32, float* dq_weight, float* dk_weight, const float* cos, const float* sin,
+             const int* positions, int rows, const Axes* axes, float eps, int interleaved, int B, int N, int H, int Hkv, int d, int dtype,
+             void* workspace, long long workspace_bytes, void* stream) {
     if (given(dq_out) != given(dq) || given(dk_out) != given(dk)) return QK_EINVAL;
     if (!given(dq)) H = 0, q_weight = nullptr, dq_weight = nullptr;
     if (!given(dk)) Hkv = 0, k_weight = nullptr, dk_weight = nullptr;
@@ -311,7 +356,8 @@ int qk_norm_rope_bwd(const qk_heads* dq_out, const qk_heads* dk_out, const qk_he
     const Grid g = grid_of((long long)B * N, H + Hkv, d, true);
     const bool sums = q_weight || k_weight;
     if (sums && (!workspace || (uintptr_t)workspace % 16 || workspace_bytes < (long long)g.x * g.y * 2 * d * 4)) return QK_EINVAL;
-    Args a = {};
+    AxesArgs a = {};
+    if (axes && !fill(&a, *axes, d)) return QK_EINVAL;
     const qk_heads* x[2] = {q, k};
     const qk_heads* dy[2] = {dq_out, dk_out};
     const qk_heads* dx[2] = {dq, dk};
@@ -332,16 +378,60 @@ int qk_norm_rope_bwd(const qk_heads* dq_out, const qk_heads* dk_out, const qk_he
     if (H && Hkv && meets(dq, dk, false, B, N, H)) return QK_EINVAL;
     a.cos = cos, a.sin = sin, a.positions = positions, a.ws = sums ? (float*)workspace : nullptr, a.tokens = (long long)B * N, a.N = N;
     a.rows = rows, a.interleaved = interleaved, a.weight_f32 = weight_f32, a.head_step = g.head_step, a.blocks_y = g.y, a.eps = eps;
-    void* list[] = {&a};
+    void* list[] = {axes ? (void*)&a : (void*)static_cast<Args*>(&a)};
+    const void* const fn = axes ? kernel<true, AxesArgs>(d, dtype, interleaved) : kernel<true, Args>(d, dtype, interleaved);
     const float* ws = a.ws;
     int blocks = g.x * g.y;
     void* sum_list[] = {&ws, &blocks, &d, &dq_weight, &dk_weight};
-    if (hipLaunchKernel(kernel<true>(d, dtype, interleaved), dim3((unsigned)blocks), dim3(256), list, 0, (hipStream_t)stream) != hipSuccess ||
+    if (hipLaunchKernel(fn, dim3((unsigned)blocks), dim3(256), list, 0, (hipStream_t)stream) != hipSuccess ||
         (sums && hipLaunchKernel((const void*)weight_sum_kernel, dim3((unsigned)d / 4), dim3(1024), sum_list, 0, (hipStream_t)stream) != hipSuccess)) {
         (void)hipGetLastError();
         return QK_ELAUNCH;
     }
     return QK_OK;
+}
+
+}  // namespace qk
+
+extern "C" {
+
+int qk_norm_rope(const qk_heads* q, const qk_heads* k, const qk_heads* q_out, const qk_heads* k_out, const void* q_weight,
+                 const void* k_weight, int weight_f32, const float* cos, const float* sin, const int* positions, int rows, float eps,
+                 int interleaved, int B, int N, int H, int Hkv, int d, int dtype, void* stream) {
+    return qk::forward(q, k, q_out, k_out, q_weight, k_weight, weight_f32, cos, sin, positions, rows, nullptr, eps, interleaved, B, N, H, Hkv, d, dtype,
+                       stream);
+}
+
+int qk_norm_rope_axes(const qk_heads* q, const qk_heads* k, const qk_heads* q_out, const qk_heads* k_out, const void* q_weight,
+                      const void* k_weight, int weight_f32, const float* cos, const float* sin, const int* positions, int rows, int axes,
+                      const unsigned char* axis_of_pair, float eps, int interleaved, int B, int N, int H, int Hkv, int d, int dtype, void* stream) {
+    const qk::Axes by = {axes, axis_of_pair};
+    return qk::forward(q, k, q_out, k_out, q_weight, k_weight, weight_f32, cos, sin, positions, rows, &by, eps, interleaved, B, N, H, Hkv, d, dtype,
+                       stream);
+}
+
+long long qk_norm_rope_bwd_workspace(int B, int N, int H, int Hkv, int d) {
+    using namespace qk;
+    if (const int rc = check(B, N, H, Hkv, d)) return rc;
+    const Grid g = grid_of((long long)B * N, H + Hkv, d, true);
+    return (long long)g.x * g.y * 2 * d * 4;
+}
+
+int qk_norm_rope_bwd(const qk_heads* dq_out, const qk_heads* dk_out, const qk_heads* q, const qk_heads* k, const qk_heads* dq,
+                     const qk_heads* dk, const void* q_weight, const void* k_weight, int weight_f32, float* dq_weight,
+                     float* dk_weight, const float* cos, const float* sin, const int* positions, int rows, float eps, int interleaved,
+                     int B, int N, int H, int Hkv, int d, int dtype, void* workspace, long long workspace_bytes, void* stream) {
+    return qk::backward(dq_out, dk_out, q, k, dq, dk, q_weight, k_weight, weight_f32, dq_weight, dk_weight, cos, sin, positions, rows, nullptr, eps,
+                        interleaved, B, N, H, Hkv, d, dtype, workspace, workspace_bytes, stream);
+}
+
+int qk_norm_rope_axes_bwd(const qk_heads* dq_out, const qk_heads* dk_out, const qk_heads* q, const qk_heads* k, const qk_heads* dq,
+                          const qk_heads* dk, const void* q_weight, const void* k_weight, int weight_f32, float* dq_weight, float* dk_weight,
+                          const float* cos, const float* sin, const int* positions, int rows, int axes, const unsigned char* axis_of_pair, float eps,
+                          int interleaved, int B, int N, int H, int Hkv, int d, int dtype, void* workspace, long long workspace_bytes, void* stream) {
+    const qk::Axes by = {axes, axis_of_pair};
+    return qk::backward(dq_out, dk_out, q, k, dq, dk, q_weight, k_weight, weight_f32, dq_weight, dk_weight, cos, sin, positions, rows, &by, eps,
+                        interleaved, B, N, H, Hkv, d, dtype, workspace, workspace_bytes, stream);
 }
 
 const char* qk_strerror(int code) {

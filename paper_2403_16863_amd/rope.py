@@ -14,7 +14,8 @@ QK_F16, QK_BF16 = 0, 1
 QK_OK, QK_EINVAL, QK_EUNSUPPORTED, QK_ELAUNCH = 0, -1, -2, -3
 
 # every symbol include/qk_rope.h declares
-SYMBOLS = ("qk_norm_rope", "qk_norm_rope_bwd", "qk_norm_rope_bwd_workspace", "qk_strerror")
+SYMBOLS = ("qk_norm_rope", "qk_norm_rope_bwd", "qk_norm_rope_axes", "qk_norm_rope_axes_bwd", "qk_norm_rope_bwd_workspace", "qk_strerror")
+NO_AXIS = 255
 
 
 class Heads(ctypes.Structure):  # qk_heads
@@ -34,6 +35,10 @@ def lib():
         L.qk_norm_rope.argtypes = [h] * 4 + [vp, vp, i, vp, vp, vp, i, f] + [i] * 7 + [vp]
         L.qk_norm_rope_bwd.restype = i
         L.qk_norm_rope_bwd.argtypes = [h] * 6 + [vp, vp, i, vp, vp, vp, vp, vp, i, f] + [i] * 7 + [vp, ctypes.c_longlong, vp]
+        L.qk_norm_rope_axes.restype = i
+        L.qk_norm_rope_axes.argtypes = [h] * 4 + [vp, vp, i, vp, vp, vp, i, i, ctypes.c_char_p, f] + [i] * 7 + [vp]
+        L.qk_norm_rope_axes_bwd.restype = i
+        L.qk_norm_rope_axes_bwd.argtypes = [h] * 6 + [vp, vp, i, vp, vp, vp, vp, vp, i, i, ctypes.c_char_p, f] + [i] * 7 + [vp, ctypes.c_longlong, vp]
         L.qk_norm_rope_bwd_workspace.restype = ctypes.c_longlong
         L.qk_norm_rope_bwd_workspace.argtypes = [i] * 5
         L.qk_strerror.restype = ctypes.c_char_p
@@ -75,7 +80,7 @@ def _heads(t):
     return Heads(None, 0, 0, 0) if t is None else Heads(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
 
 
-def _common(like, cos, sin, positions, weights, given):
+def _common(like, cos, sin, positions, weights, given, axes=None):
     import torch
     for name, t in given:
         if t is None:
@@ -87,8 +92,16 @@ def _common(like, cos, sin, positions, weights, given):
     if like.dtype not in (torch.float16, torch.bfloat16):
         raise TypeError(f"queries and keys must be float16 or bfloat16, got {like.dtype}")
     B, N, _, d = like.shape
-    if positions.dtype != torch.int32 or tuple(positions.shape) != (B, N) or not positions.is_contiguous():
-        raise ValueError("positions must be contiguous int32 [B,N]")
+    if axes is None:
+        if positions.dtype != torch.int32 or tuple(positions.shape) != (B, N) or not positions.is_contiguous():
+            raise ValueError("positions must be contiguous int32 [B,N]")
+    else:
+        if positions.dtype != torch.int32 or positions.dim() != 3 or tuple(positions.shape[:2]) != (B, N) or not positions.is_contiguous():
+            raise ValueError("positions must be contiguous int32 [B,N,axes]")
+        if not isinstance(axes, bytes) or len(axes) != d // 2:
+            raise ValueError(f"axes must be d/2 = {d // 2} bytes, one for each pair (axes_of_pairs makes them)")
+        if not 1 <= positions.shape[2] <= 4 or any(a >= positions.shape[2] and a != NO_AXIS for a in axes):
+            raise ValueError("positions must have 1 to 4 axes, and axes name one of them, or NO_AXIS, for each pair")
     for name, t in (("cos", cos), ("sin", sin)):
         if t.dtype != torch.float32 or t.dim() != 2 or t.shape[1] != d // 2 or t.shape != cos.shape or not t.is_contiguous():
             raise ValueError(f"{name} must be contiguous float32 [rows,d/2]")
@@ -118,6 +131,7 @@ def _first(name):
 
 
 _plain_norm_rope, _plain_norm_rope_bwd = _first("norm_rope"), _first("norm_rope_bwd")
+_plain_norm_rope_axes, _plain_norm_rope_axes_bwd = _first("norm_rope_axes"), _first("norm_rope_axes_bwd")
 
 
 def qk_norm_rope(q, k, q_out, k_out, cos, sin, positions, q_weight=None, k_weight=None, eps: float = 1e-6, interleaved: bool = False,
@@ -131,7 +145,11 @@ def qk_norm_rope(q, k, q_out, k_out, cos, sin, positions, q_weight=None, k_weigh
         return
     if rc < 0:
         raise RopeError(rc, "qk_norm_rope")
-    # not a plain call: the steps one by one, each of which says what it refuses
+    _forward("qk_norm_rope", q, k, q_out, k_out, cos, sin, positions, None, q_weight, k_weight, eps, interleaved, stream)
+
+
+def _forward(what, q, k, q_out, k_out, cos, sin, positions, axes, q_weight, k_weight, eps, interleaved, stream) -> None:
+    """Not a plain call: the steps one by one, each of which says what it refuses."""
     import torch
     like = q if q is not None else k
     if like is None or (q is None) != (q_out is None) or (k is None) != (k_out is None):
@@ -141,15 +159,48 @@ def qk_norm_rope(q, k, q_out, k_out, cos, sin, positions, q_weight=None, k_weigh
         _check_heads(name, t, like, heads)
     f32, dt = _common(like, cos, sin, positions, (q_weight, k_weight),
                       (("q", q), ("k", k), ("q_out", q_out), ("k_out", k_out), ("cos", cos), ("sin", sin), ("positions", positions),
-                       ("q_weight", q_weight), ("k_weight", k_weight)))
+                       ("q_weight", q_weight), ("k_weight", k_weight)), axes)
     B, N, _, d = like.shape
-    _fit("qk_norm_rope", B, N, H, Hkv, cos.shape[0])
+    _fit(what, B, N, H, Hkv, cos.shape[0])
     hs = [_heads(t) for t in (q, k, q_out, k_out)]
+    by = () if axes is None else (positions.shape[2], axes)
     with torch.cuda.device(like.device):
-        rc = lib().qk_norm_rope(*hs, _ptr(q_weight), _ptr(k_weight), f32, cos.data_ptr(), sin.data_ptr(), positions.data_ptr(), cos.shape[0],
-                                float(eps), int(bool(interleaved)), B, N, H, Hkv, d, dt, _stream(stream, like.device))
+        rc = getattr(lib(), what)(*hs, _ptr(q_weight), _ptr(k_weight), f32, cos.data_ptr(), sin.data_ptr(), positions.data_ptr(), cos.shape[0], *by,
+                                  float(eps), int(bool(interleaved)), B, N, H, Hkv, d, dt, _stream(stream, like.device))
     if rc != QK_OK:
-        raise RopeError(rc, "qk_norm_rope")
+        raise RopeError(rc, what)
+
+
+def axes_of_pairs(sections, d: int, alternating: bool = False) -> bytes:
+    """The axis of each of the d/2 pairs, as qk_norm_rope_axes takes them: sections[a] pairs turn by axis a, one axis after the other or, alternating, the
+    axes taking turns until their shares are used up; pairs behind the last are not turned."""
+    left = [int(n) for n in sections]
+    if not 1 <= len(left) <= 4 or min(left) < 0 or sum(left) > d // 2:
+        raise ValueError(f"sections must be 1 to 4 numbers of pairs, {d // 2} in all at most")
+    found = []
+    if alternating:
+        while any(left):
+            for a, n in enumerate(left):
+                if n:
+                    found.append(a)
+                    left[a] -= 1
+    else:
+        for a, n in enumerate(left):
+            found += [a] * n
+    return bytes(found + [NO_AXIS] * (d // 2 - len(found)))
+
+
+def qk_norm_rope_axes(q, k, q_out, k_out, cos, sin, positions, axes, q_weight=None, k_weight=None, eps: float = 1e-6, interleaved: bool = False,
+                      stream=None) -> None:
+    """qk_norm_rope with positions on several axes, int32 [B,N,axes] with 1 to 4 of them (time, height and width of a video's patches, say): each pair of
+    channels turns by the row of cos and sin that the position on its own axis names.  axes: the axis of each of the d/2 pairs, as bytes
+    (axes_of_pairs makes them), NO_AXIS for a pair that is not turned."""
+    rc = _plain_norm_rope_axes(q, k, q_out, k_out, cos, sin, positions, axes, q_weight, k_weight, eps, interleaved, stream)
+    if not rc:
+        return
+    if rc < 0:
+        raise RopeError(rc, "qk_norm_rope_axes")
+    _forward("qk_norm_rope_axes", q, k, q_out, k_out, cos, sin, positions, axes, q_weight, k_weight, eps, interleaved, stream)
 
 
 def qk_norm_rope_bwd_workspace(B: int, N: int, H: int, Hkv: int, d: int) -> int:
@@ -175,7 +226,13 @@ def qk_norm_rope_bwd(dq_out, dk_out, q, k, dq, dk, cos, sin, positions, q_weight
         return
     if rc < 0:
         raise RopeError(rc, "qk_norm_rope_bwd")
-    # not a plain call: the steps one by one, each of which says what it refuses
+    _backward("qk_norm_rope_bwd", dq_out, dk_out, q, k, dq, dk, cos, sin, positions, None, q_weight, k_weight, dq_weight, dk_weight, eps, interleaved,
+              workspace, stream)
+
+
+def _backward(what, dq_out, dk_out, q, k, dq, dk, cos, sin, positions, axes, q_weight, k_weight, dq_weight, dk_weight, eps, interleaved, workspace,
+              stream) -> None:
+    """Not a plain call: the steps one by one, each of which says what it refuses."""
     import torch
     like = dq_out if dq_out is not None else dk_out
     if like is None or (dq_out is None) != (dq is None) or (dk_out is None) != (dk is None):
@@ -191,9 +248,9 @@ def qk_norm_rope_bwd(dq_out, dk_out, q, k, dq, dk, cos, sin, positions, q_weight
     f32, dt = _common(like, cos, sin, positions, (q_weight, k_weight),
                       (("dq_out", dq_out), ("dk_out", dk_out), ("q", q), ("k", k), ("dq", dq), ("dk", dk), ("cos", cos), ("sin", sin),
                        ("positions", positions), ("q_weight", q_weight), ("k_weight", k_weight), ("dq_weight", dq_weight),
-                       ("dk_weight", dk_weight), ("workspace", workspace)))
+                       ("dk_weight", dk_weight), ("workspace", workspace)), axes)
     B, N, _, d = like.shape
-    _fit("qk_norm_rope_bwd", B, N, H, Hkv, cos.shape[0])
+    _fit(what, B, N, H, Hkv, cos.shape[0])
     for w in (dq_weight, dk_weight):
         if w is not None and (w.dtype != torch.float32 or tuple(w.shape) != (d,) or not w.is_contiguous()):
             raise ValueError("gradients of weights must be contiguous float32 [d]")
@@ -207,9 +264,23 @@ def qk_norm_rope_bwd(dq_out, dk_out, q, k, dq, dk, cos, sin, positions, q_weight
                 raise ValueError("a stream that is not torch's current one, or a recording that torch did not begin, needs a workspace")
         elif not workspace.is_contiguous() or workspace.numel() * workspace.element_size() < need:
             raise ValueError(f"workspace must be contiguous with {need} bytes")
+    by = () if axes is None else (positions.shape[2], axes)
     with torch.cuda.device(like.device):
-        rc = lib().qk_norm_rope_bwd(*hs, _ptr(q_weight), _ptr(k_weight), f32, _ptr(dq_weight), _ptr(dk_weight), cos.data_ptr(), sin.data_ptr(),
-                                    positions.data_ptr(), cos.shape[0], float(eps), int(bool(interleaved)), B, N, H, Hkv, d, dt,
-                                    _ptr(workspace) if need else None, need, st)
+        rc = getattr(lib(), what)(*hs, _ptr(q_weight), _ptr(k_weight), f32, _ptr(dq_weight), _ptr(dk_weight), cos.data_ptr(), sin.data_ptr(),
+                                  positions.data_ptr(), cos.shape[0], *by, float(eps), int(bool(interleaved)), B, N, H, Hkv, d, dt,
+                                  _ptr(workspace) if need else None, need, st)
     if rc != QK_OK:
-        raise RopeError(rc, "qk_norm_rope_bwd")
+        raise RopeError(rc, what)
+
+
+def qk_norm_rope_axes_bwd(dq_out, dk_out, q, k, dq, dk, cos, sin, positions, axes, q_weight=None, k_weight=None, dq_weight=None, dk_weight=None,
+                          eps: float = 1e-6, interleaved: bool = False, workspace=None, stream=None) -> None:
+    """The gradients of qk_norm_rope_axes, as qk_norm_rope_bwd gives those of qk_norm_rope (its workspace is the same)."""
+    rc = _plain_norm_rope_axes_bwd(dq_out, dk_out, q, k, dq, dk, cos, sin, positions, axes, q_weight, k_weight, dq_weight, dk_weight, eps, interleaved,
+                                   workspace, stream)
+    if not rc:
+        return
+    if rc < 0:
+        raise RopeError(rc, "qk_norm_rope_axes_bwd")
+    _backward("qk_norm_rope_axes_bwd", dq_out, dk_out, q, k, dq, dk, cos, sin, positions, axes, q_weight, k_weight, dq_weight, dk_weight, eps, interleaved,
+              workspace, stream)
