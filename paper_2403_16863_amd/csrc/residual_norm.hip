@@ -550,8 +550,8 @@ extern "C" {
 int residual_norm(const norm_tokens* x, const norm_tokens* h, const norm_tokens* y, const norm_tokens* z, const norm_vectors* vectors, int B,
                   int N, int C, int dtype, void* stream) {
     using namespace stream_norm;
-    if (const int rc = check_vectors(vectors, B, C, dtype)) return rc;
     if (const int rc = check_sizes(B, N, C)) return rc;
+    if (const int rc = check_vectors(vectors, B, C, dtype)) return rc;
     const norm_vectors& v = *vectors;
     if (!given(x) || (!given(y) && !given(z)) || given(z) != (v.pre_weight != nullptr)) return NORM_EINVAL;
     if (!given(h) && (given(y) || v.gate || v.post_weight || v.alpha != 1.f)) return NORM_EINVAL;
@@ -586,8 +586,8 @@ int residual_norm_bwd(const norm_tokens* dy, const norm_tokens* dz, const norm_t
                       const norm_tokens* dh, const norm_vectors* vectors, float* dgate, float* dpost_weight, float* dpre_weight, int B, int N,
                       int C, int dtype, void* workspace, long long workspace_bytes, void* stream) {
     using namespace stream_norm;
-    if (const int rc = check_vectors(vectors, B, C, dtype)) return rc;
     if (const int rc = check_sizes(B, N, C)) return rc;
+    if (const int rc = check_vectors(vectors, B, C, dtype)) return rc;
     const norm_vectors& v = *vectors;
     const bool need_h = v.gate || v.post_weight, sequences = by_sequence(&v);
     if ((!given(dy) && !given(dz)) || (!given(dx) && !given(dh)) || given(dz) != (v.pre_weight != nullptr) || (given(dz) && !given(y)) || (need_h && !given(h)))
