@@ -14,6 +14,10 @@ template <class T>
 __global__ __launch_bounds__(64) void join_kernel(const float* parts, Args p, int ranges, unsigned chunks) {
     const unsigned i = blockIdx.x * 64 + threadIdx.x;
     if (i >= chunks) return;
+    const unsigned row = (unsigned)p.N / 8, m = i / row, n = (i - m * row) * 8;
+    float bias[8];
+    load_bias<T>(p.e, (int)n, true, bias);
+    const u32x4 residual = load_residual(p.e, (int)m, (int)n, true);
     const f32x4* src = reinterpret_cast<const f32x4*>(parts) + (size_t)i * 2;
     f32x4 x = src[0], y = src[1];
 #pragma unroll 4
@@ -23,8 +27,7 @@ __global__ __launch_bounds__(64) void join_kernel(const float* parts, Args p, in
         y += src[1];
     }
     float v[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
-    const unsigned row = (unsigned)p.N / 8, m = i / row;
-    finish8<T>(p.e, (uint16_t*)p.out, p.ldo, (int)m, (int)(i - m * row) * 8, v);
+    finish8<T>(p.e, (uint16_t*)p.out, p.ldo, (int)m, (int)n, v, bias, residual);
 }
 
 // dz = dy act'(pre), rounded, and the rows' sums for dbias, in one pass over dy and pre: memory binds.  A workgroup has 256 / lanes rows of `lanes` vectors of 8

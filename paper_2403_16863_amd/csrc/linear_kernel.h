@@ -59,9 +59,11 @@ __device__ __forceinline__ u32x4 pack8(const float* x) {
 // The activations of eight values.  In 32 bits with the hardware's exponential (2^x) and reciprocal, each good to a step or so: the results
 // are rounded to 16 bits.  z = -inf gives NaN in silu and both gelu, -inf times 0, as their formulas do.
 __device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.4426950408889634f)); }
-// Twice the argument of the tanh form.  tanh(u / 2) = 2 sigmoid(u) - 1, so the form is z sigmoid(u): one exponential, and no
-// difference of near values where the result is small.
-__device__ __forceinline__ float tanh_argument(float z) { return 1.5957691216057308f * z * fmaf(0.044715f * z, z, 1.f); }
+// sigmoid(2 v) of the tanh form's argument v = sqrt(2 / pi) (z + 0.044715 z^3): tanh v = 2 sigmoid(2 v) - 1, so the form is z times it: one
+// exponential, and no difference of near values where the result is small.  (The constants times -log2 e.)
+__device__ __forceinline__ float sigmoid_of_cubic(float z) {
+    return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * fmaf(z * z, -0.10294324f, -2.3022082f)));
+}
 // The normal distribution's integral from -inf to z, and in *density its density.  With x = |z| / sqrt 2 and t = 1 / (1 + 0.38 x), e^(x^2) erfc(x) is a
 // polynomial in t (Hastings' form) to 2e-6 of itself, its coefficients fitted to the least relative error over 0 .. 20: the tail
 // keeps its digits for negative z, where 1 + erf loses them, at a third of the library function's instructions.
@@ -93,7 +95,7 @@ __device__ __forceinline__ void act8(float* v, int kind) {
         }
     } else if (kind == GELU_TANH) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] *= sigmoid(tanh_argument(v[i]));
+        for (int i = 0; i < 8; ++i) v[i] *= sigmoid_of_cubic(v[i]);
     }
 }
 
@@ -118,7 +120,7 @@ __device__ __forceinline__ void act_slope8(const float* v, float* g, int kind) {
     } else if (kind == GELU_TANH) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float p = sigmoid(tanh_argument(v[i]));
+            const float p = sigmoid_of_cubic(v[i]);
             g[i] *= p * fmaf(1.5957691216057308f * v[i] * (1.f - p), fmaf(3.f * 0.044715f * v[i], v[i], 1.f), 1.f);
         }
     }
@@ -127,7 +129,7 @@ __device__ __forceinline__ void act_slope8(const float* v, float* g, int kind) {
 template <int BM_, int BN_, int BK_, int WM_, int WN_, int WK_, int NB_, int OCC_>
 struct Tile {
     static constexpr int BM = BM_, BN = BN_;  // tile of C of one workgroup
-    static constexpr int BK = BK_;            // k extent of one stage: 32 or 64
+    static constexpr int BK = BK_;            // k extent of one stage
     static constexpr int WM = WM_, WN = WN_;  // its waves, as a grid over that tile
     static constexpr int WK = WK_;            // groups of WM x WN waves that split k between them
     static constexpr int NB = NB_;            // stages of a ring
@@ -152,25 +154,36 @@ struct Args {
     Epilogue e;
 };
 
+// What the epilogue reads for eight consecutive columns of a row.  All of it is asked for ahead of the first store, behind which the compiler, which does
+// not know that they do not meet, would keep it: a load's time for each store.
+template <class T>
+__device__ __forceinline__ void load_bias(const Epilogue& e, int n, bool in, float* b) {
+    if (in && e.bias && e.bias_f32) {
+        const float4 lo = ((const float4*)((const float*)e.bias + n))[0], hi = ((const float4*)((const float*)e.bias + n))[1];
+        b[0] = lo.x, b[1] = lo.y, b[2] = lo.z, b[3] = lo.w, b[4] = hi.x, b[5] = hi.y, b[6] = hi.z, b[7] = hi.w;
+    } else if (in && e.bias) {
+        unpack8<T>(*(const u32x4*)((const uint16_t*)e.bias + n), b);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) b[i] = 0;
+    }
+}
+__device__ __forceinline__ u32x4 load_residual(const Epilogue& e, int m, int n, bool in) {
+    return in && e.residual ? *(const u32x4*)(e.residual + (size_t)m * e.ldr + n) : u32x4{0, 0, 0, 0};
+}
+
 // Eight consecutive values of one row of C: bias, activation, residual, one rounding.
 template <class T>
-__device__ __forceinline__ void finish8(const Epilogue& e, uint16_t* out, int ldo, int m, int n, float* v) {
-    if (e.bias) {
-        float b[8];
-        if (e.bias_f32) {
-            const float4 lo = ((const float4*)((const float*)e.bias + n))[0], hi = ((const float4*)((const float*)e.bias + n))[1];
-            b[0] = lo.x, b[1] = lo.y, b[2] = lo.z, b[3] = lo.w, b[4] = hi.x, b[5] = hi.y, b[6] = hi.z, b[7] = hi.w;
-        } else {
-            unpack8<T>(*(const u32x4*)((const uint16_t*)e.bias + n), b);
-        }
+__device__ __forceinline__ void finish8(const Epilogue& e, uint16_t* out, int ldo, int m, int n, float* v, const float* bias, u32x4 residual) {
+    if (e.bias) {  // (a sum without one keeps the sign of a zero)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] += b[i];
+        for (int i = 0; i < 8; ++i) v[i] += bias[i];
     }
     if (e.pre) *(u32x4*)(e.pre + (size_t)m * e.ldp + n) = pack8<T>(v);
     act8(v, e.act);
     if (e.residual) {
         float r[8];
-        unpack8<T>(*(const u32x4*)(e.residual + (size_t)m * e.ldr + n), r);
+        unpack8<T>(residual, r);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] += r[i];
     }
@@ -221,17 +234,26 @@ struct Piece {
         const int i16 = lane & 15, row = 8 * (lane >> 4) + (i16 >> 2);
         return (row + 32 * j) * (R * 2) + (((at >> 4) ^ code(row)) * 32) + (i16 & 3) * 8;
     }
-    static __device__ __forceinline__ u32x4 read(unsigned at) {
+    // The fragment `offset` bytes (a constant) behind a lane's address.
+    static __device__ __forceinline__ u32x4 read(unsigned at, int offset) {
+        typedef const char __attribute__((address_space(3))) * lds_char_ptr;
+        const lds_char_ptr p = (lds_char_ptr)(unsigned long)at + offset;
         if constexpr (ALONG) {
             typedef const u32x4 __attribute__((address_space(3))) * lds_u32x4_ptr;
-            return *(lds_u32x4_ptr)(unsigned long)at;
+            return *(lds_u32x4_ptr)p;
         } else {
-            const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(unsigned long)at));
-            const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(unsigned long)(at + 4 * R * 2)));
+            const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)p));
+            const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(p + 4 * R * 2)));
             return u32x4{lo[0], lo[1], hi[0], hi[1]};
         }
     }
 };
+
+// 16 bytes a lane from global memory to LDS, OFFSET bytes behind `lds`.
+template <int OFFSET>
+__device__ __forceinline__ void buffer_to_lds(u32x4 rsrc, unsigned voff, unsigned lds) {
+    asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(voff), "s"(rsrc), "s"(lds), "n"(OFFSET) : "memory", "m0", "scc");
+}
 
 template <class T, class TL, bool A_ALONG, bool B_ALONG, bool PARTS>
 __global__ __launch_bounds__(TL::WM * TL::WN * TL::WK * 64, (TL::OCC * TL::WM * TL::WN * TL::WK + 3) / 4) void product_kernel(Args p) {
@@ -241,6 +263,7 @@ __global__ __launch_bounds__(TL::WM * TL::WN * TL::WK * 64, (TL::OCC * TL::WM * 
     using PB = Piece<B_ALONG, BN, BK, NW>;
     constexpr int LA = PA::LOADS, LB = PB::LOADS, LPS = LA + LB;
     constexpr int RING = NB * (PA::BYTES + PB::BYTES);
+    static_assert(KS == 2, "fragments of a stage's two steps take turns");
     static_assert(NT % 2 == 0, "C is stored in pairs of 16-column tiles");
     static_assert(NB >= 2 && (NB - 1) * LPS <= 63, "the counted waits must fit s_waitcnt's field");
     static_assert(WK == 1 || RING >= BM * BN * 4, "a ring also holds its group's partial sums");
@@ -278,30 +301,35 @@ __global__ __launch_bounds__(TL::WM * TL::WN * TL::WK * 64, (TL::OCC * TL::WM * 
     int left = K1 - k0;  // values of k behind the first of the next stage to be requested
     u32x4 ra, rb;
     auto next_stage = [&](int t) __attribute__((always_inline)) {
-        if (left < BK) pa.clip(left), pb.clip(left);  // the last, partial stage: chunks past the end deliver zeros on both sides
+        if (left < BK) {  // the last, partial stage: chunks past the end deliver zeros on both sides
+            asm volatile("");  // (a branch: as selections the clipping would cost every stage)
+            pa.clip(left), pb.clip(left);
+        }
         const unsigned size = t < nkt ? kBufferSize : 0u;
         ra = attn::buffer_resource(pa.p, size), rb = attn::buffer_resource(pb.p, size);
         pa.advance(step, p.lda), pb.advance(step, p.ldb);
         left -= step;
     };
-    unsigned lbuf = 0;  // buffer of the stage being requested
+    unsigned load_a = lds_a + wave * (LA * 1024), load_b = lds_b + wave * (LB * 1024);  // where the stage being requested goes
     auto issue = [&](auto l_c) __attribute__((always_inline)) {
         constexpr int l = decltype(l_c)::value;
-        if constexpr (l < LA) attn::buffer_to_lds_16(ra, pa.voff[l], lds_a + lbuf * PA::BYTES + (wave * LA + l) * 1024);
-        else attn::buffer_to_lds_16(rb, pb.voff[l - LA], lds_b + lbuf * PB::BYTES + (wave * LB + l - LA) * 1024);
+        if constexpr (l < LA) buffer_to_lds<l * 1024>(ra, pa.voff[l], load_a);
+        else buffer_to_lds<(l - LA) * 1024>(rb, pb.voff[l - LA], load_b);
     };
 
-    // k along the rows: one address for each step, fragments 16 rows apart; by rows of k: one for each fragment, steps 32 rows apart
-    unsigned a_base[A_ALONG ? KS : MT], b_base[B_ALONG ? KS : NT];
+    // k along the rows: one address for each step, fragments 16 rows apart; by rows of k: one for each fragment, steps 32 rows apart.  They follow
+    // the stage whose fragments are read, so that everything else of an address is a constant of the instruction.
+    constexpr int NBA = A_ALONG ? KS : MT, NBB = B_ALONG ? KS : NT;
+    unsigned a_base[NBA], b_base[NBB];
 #pragma unroll
-    for (int i = 0; i < (A_ALONG ? KS : MT); ++i) a_base[i] = lds_a + (A_ALONG ? PA::address(wm * TM, i, lane) : PA::address(wm * TM + 16 * i, 0, lane));
+    for (int i = 0; i < NBA; ++i) a_base[i] = lds_a + (A_ALONG ? PA::address(wm * TM, i, lane) : PA::address(wm * TM + 16 * i, 0, lane));
 #pragma unroll
-    for (int i = 0; i < (B_ALONG ? KS : NT); ++i) b_base[i] = lds_b + (B_ALONG ? PB::address(wn * TN, i, lane) : PB::address(wn * TN + 16 * i, 0, lane));
-    auto read_a = [&](int mt, int j, unsigned buf) __attribute__((always_inline)) -> u32x4 {
-        return PA::read(buf * PA::BYTES + (A_ALONG ? a_base[j] + mt * 16 * (BK * 2) : a_base[mt] + j * 32 * (BM * 2)));
+    for (int i = 0; i < NBB; ++i) b_base[i] = lds_b + (B_ALONG ? PB::address(wn * TN, i, lane) : PB::address(wn * TN + 16 * i, 0, lane));
+    auto read_a = [&](int mt, int j) __attribute__((always_inline)) -> u32x4 {
+        return PA::read(a_base[A_ALONG ? j : mt], A_ALONG ? mt * 16 * (BK * 2) : j * 32 * (BM * 2));
     };
-    auto read_b = [&](int nt, int j, unsigned buf) __attribute__((always_inline)) -> u32x4 {
-        return PB::read(buf * PB::BYTES + (B_ALONG ? b_base[j] + nt * 16 * (BK * 2) : b_base[nt] + j * 32 * (BN * 2)));
+    auto read_b = [&](int nt, int j) __attribute__((always_inline)) -> u32x4 {
+        return PB::read(b_base[B_ALONG ? j : nt], B_ALONG ? nt * 16 * (BK * 2) : j * 32 * (BN * 2));
     };
 
     f32x4 acc[MT][NT];
@@ -310,79 +338,83 @@ __global__ __launch_bounds__(TL::WM * TL::WN * TL::WK * 64, (TL::OCC * TL::WM * 
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) acc[mt][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    // The loads l = 0 .. LPS-1 of a stage go out one by one between the MFMAs, from the step behind the barrier on and through the steps
-    // ahead of the next one; load l behind MFMA number slot(l).
-    constexpr int FIRST = NB == 2 ? 0 : KS == 1 ? MT * NT / 2 : MT * NT / 4, SPAN = (NB == 2 ? 1 : KS) * MT * NT;
-    auto slot = [](int l) constexpr { return FIRST + l * (SPAN - FIRST) / LPS; };
-    auto first_loads = [=]() constexpr { int n = 0; for (int l = 0; l < LPS; ++l) n += slot(l) < MT * NT; return n; };
+    // A stage is 2 S products, S to a step; where its other work goes, in products from its first:
+    //   0 ..      the second step's fragments are read
+    //   FREED     all of the stage's fragments are in registers, in all waves: its buffer takes the loads of stage t + NB from here on, load l at slot(l)
+    //   LANDED    the loads of stage t + 1 are there, of all waves; its first step's fragments are read
+    // With three buffers and more both are one barrier, ahead of the second step.  With two the loads have to go out and land within the stage between two such
+    // barriers, and half of that is the time that 64 KB take to come; a barrier of its own for each gives them the one and a half stages from FREED to LANDED.
+    constexpr int S = MT * NT, R = MT + NT, READS = NB == 2 ? S / 4 : S / 2 > R ? R : (S + 1) / 2;  // (products among which a step's fragments are read)
+    constexpr int FREED = NB == 2 ? S * 3 / 8 : S, LANDED = NB == 2 ? S + S * 5 / 8 : S;
+    constexpr int FIRST = NB == 2 ? FREED : S + S / 4, SPAN = NB == 2 ? S * 3 / 2 : 2 * S - S / 4;
+    auto slot = [](int l) constexpr { return FIRST + l * SPAN / LPS; };
+    auto before = [=](int at) constexpr { int n = 0; for (int l = 0; l < LPS; ++l) n += slot(l) < at; return n; };
+    static_assert(NB > 2 || (FREED > READS && FIRST + SPAN <= 2 * S && LANDED + READS < 2 * S), "a stage's own work ends with it");
 #pragma unroll
     for (int t = 0; t < NB; ++t) {
         next_stage(t);
-        lbuf = t;
         attn::static_for<LPS>([&](auto l_c) __attribute__((always_inline)) {
-            if (t < NB - 1 || slot(decltype(l_c)::value) < MT * NT) issue(l_c);
+            if (NB == 2 || t < NB - 1 || slot(decltype(l_c)::value) < 2 * S) issue(l_c);
         });
+        if (t < NB - 1) load_a += PA::BYTES, load_b += PB::BYTES;
     }
     u32x4 fa[2][MT], fb[2][NT];
     auto meet = []() __attribute__((always_inline)) { if constexpr (NW > 1) asm volatile("s_barrier" ::: "memory"); };
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NB - 2) * LPS + first_loads()) : "memory");
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(NB == 2 ? LPS : (NB - 2) * LPS + before(2 * S)) : "memory");
     meet();
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) fb[0][nt] = read_b(nt, 0, 0);
+    for (int nt = 0; nt < NT; ++nt) fb[0][nt] = read_b(nt, 0);
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) fa[0][mt] = read_a(mt, 0, 0);
+    for (int mt = 0; mt < MT; ++mt) fa[0][mt] = read_a(mt, 0);
 
     unsigned buf = 0;  // t % NB
-    auto stage = [&](auto par_c, int t) __attribute__((always_inline)) {
+    for (int t = 0; t < nkt; ++t) {
         const unsigned nbuf = buf + 1 == NB ? 0 : buf + 1;
-        attn::static_for<KS>([&](auto j_c) __attribute__((always_inline)) {
-            constexpr int j = decltype(j_c)::value, P = (decltype(par_c)::value + j) & 1, Q = P ^ 1;
-            constexpr bool LAST = j == KS - 1;
-            constexpr int nj = LAST ? 0 : j + 1;
-            const unsigned rbuf = LAST ? nbuf : buf;
-            if constexpr (LAST) {
-                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((NB - 2) * LPS) : "memory");
+        attn::static_for<2 * S>([&](auto at_c) __attribute__((always_inline)) {
+            constexpr int at = decltype(at_c)::value, P = at / S, i = at % S, mt = i / NT, nt = i % NT;
+            if constexpr (at == FREED && NB == 2) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
                 meet();
-                next_stage(t + NB);
-                lbuf = buf;
             }
-            attn::static_for<MT * NT>([&](auto i_c) __attribute__((always_inline)) {
-                constexpr int i = decltype(i_c)::value, mt = i / NT, nt = i % NT;
-                acc[mt][nt] = T::mfma(fb[P][nt], fa[P][mt], acc[mt][nt]);
-                // fragment reads spread over the first half of the step, loads over the second
-                constexpr int R = MT + NT, STEPS = MT * NT / 2 > R ? R : (MT * NT + 1) / 2;
-                attn::static_for<R>([&](auto r_c) __attribute__((always_inline)) {
-                    constexpr int q = decltype(r_c)::value;
-                    if constexpr (i == q * STEPS / R) {
-                        if constexpr (q < NT) fb[Q][q] = read_b(q, nj, rbuf);
-                        else fa[Q][q - NT] = read_a(q - NT, nj, rbuf);
-                    }
-                });
-                attn::static_for<LPS>([&](auto l_c) __attribute__((always_inline)) {
-                    if constexpr (slot(decltype(l_c)::value) == (LAST ? 0 : j + 1) * MT * NT + i) issue(l_c);
-                });
-                __builtin_amdgcn_sched_barrier(0);
+            if constexpr (at == LANDED) {
+                if constexpr (NB == 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(before(LANDED)) : "memory");
+                else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((NB - 2) * LPS) : "memory");
+                meet();
+                const unsigned on_a = nbuf ? PA::BYTES : -(NB - 1) * PA::BYTES, on_b = nbuf ? PB::BYTES : -(NB - 1) * PB::BYTES;
+#pragma unroll
+                for (int n = 0; n < NBA; ++n) a_base[n] += on_a;
+#pragma unroll
+                for (int n = 0; n < NBB; ++n) b_base[n] += on_b;
+            }
+            if constexpr (at == FREED) {
+                next_stage(t + NB);
+                load_a = lds_a + wave * (LA * 1024) + buf * PA::BYTES, load_b = lds_b + wave * (LB * 1024) + buf * PB::BYTES;
+            }
+            acc[mt][nt] = T::mfma(fb[P][nt], fa[P][mt], acc[mt][nt]);
+            attn::static_for<R>([&](auto r_c) __attribute__((always_inline)) {
+                constexpr int q = decltype(r_c)::value, when = q * READS / R;
+                if constexpr (at == when || at == LANDED + when) {
+                    if constexpr (q < NT) fb[at == when][q] = read_b(q, at == when);
+                    else fa[at == when][q - NT] = read_a(q - NT, at == when);
+                }
             });
+            attn::static_for<LPS>([&](auto l_c) __attribute__((always_inline)) {
+                if constexpr (slot(decltype(l_c)::value) % (2 * S) == at) issue(l_c);
+            });
+            __builtin_amdgcn_sched_barrier(0);
         });
         buf = nbuf;
-    };
-    if constexpr (KS % 2 == 0) {
-        for (int t = 0; t < nkt; ++t) stage(std::integral_constant<int, 0>{}, t);
-    } else {
-        for (int t = 0; t < nkt; t += 2) {
-            stage(std::integral_constant<int, 0>{}, t);
-            stage(std::integral_constant<int, 1>{}, t + 1);
-        }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (stages past the end were requested empty)
 
     // ---- a lane holds n = 4g .. 4g+3 of one row of each 16 x 16 tile; exchanged between the odd and even 16-lane groups of two
     // neighbouring tiles it has eight consecutive n.
     const int g = lane >> 4;
-    auto store_pair = [&](int mt, int nt, f32x4 x, f32x4 y) __attribute__((always_inline)) {
-        const int m = m0 + wm * TM + mt * 16 + (lane & 15);
+    auto row_of = [&](int mt) __attribute__((always_inline)) { return m0 + wm * TM + mt * 16 + (lane & 15); };
+    auto column_of = [&](int nt) __attribute__((always_inline)) { return n0 + wn * TN + nt * 16 + (PARTS ? g * 4 : (g & 1) * 16 + (g >> 1) * 8); };
+    auto store_pair = [&](int mt, int nt, f32x4 x, f32x4 y, const float* bias, u32x4 residual) __attribute__((always_inline)) {
+        const int m = row_of(mt), n = column_of(nt);
         if constexpr (PARTS) {
-            const int n = n0 + wn * TN + nt * 16 + g * 4;
             float* const row = (float*)p.out + ((size_t)range * M + m) * N;
             if (m < M && n < N) *(f32x4*)(row + n) = x;
             if (m < M && n + 16 < N) *(f32x4*)(row + n + 16) = y;
@@ -394,23 +426,43 @@ __global__ __launch_bounds__(TL::WM * TL::WN * TL::WK * 64, (TL::OCC * TL::WM * 
             const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(x[i]), __float_as_uint(y[i]), false, false);
             v[i] = __uint_as_float(s[0]), v[4 + i] = __uint_as_float(s[1]);
         }
-        const int n = n0 + wn * TN + nt * 16 + (g & 1) * 16 + (g >> 1) * 8;
-        if (m < M && n < N) finish8<T>(p.e, (uint16_t*)p.out, p.ldo, m, n, v);
+        if (m < M && n < N) finish8<T>(p.e, (uint16_t*)p.out, p.ldo, m, n, v, bias, residual);
     };
     if constexpr (WK == 1) {
+        float bias[NT / 2][8];
+        u32x4 residual[MT][NT / 2];
+        if constexpr (!PARTS) {
+#pragma unroll
+            for (int q = 0; q < NT / 2; ++q) {
+                const int n = column_of(2 * q);
+                load_bias<T>(p.e, n, n < N, bias[q]);
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) residual[mt][q] = load_residual(p.e, row_of(mt), n, n < N && row_of(mt) < M);
+            }
+        }
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-            for (int nt = 0; nt < NT; nt += 2) store_pair(mt, nt, acc[mt][nt], acc[mt][nt + 1]);
+            for (int nt = 0; nt < NT; nt += 2) store_pair(mt, nt, acc[mt][nt], acc[mt][nt + 1], bias[nt / 2], residual[mt][nt / 2]);
     } else {
-        constexpr int PAIRS = MT * NT / 2;
+        constexpr int PAIRS = MT * NT / 2, MINE = (PAIRS + WK - 1) / WK;
         if constexpr (NW > 1) __syncthreads();  // the ring is shared by the group's waves
         f32x4* const mine = reinterpret_cast<f32x4*>(smem_b + wk * RING + wave * (TM * TN * 4)) + lane;
 #pragma unroll
         for (int i = 0; i < MT * NT; ++i) mine[i * 64] = acc[i / NT][i % NT];
+        float bias[MINE][8];
+        u32x4 residual[MINE];
+        if constexpr (!PARTS) {
+#pragma unroll
+            for (int q = 0; q < MINE; ++q) {
+                const int pr = q * WK + wk, m = row_of(pr / (NT / 2)), n = column_of(pr % (NT / 2) * 2);
+                load_bias<T>(p.e, n, pr < PAIRS && n < N, bias[q]);
+                residual[q] = load_residual(p.e, m, n, pr < PAIRS && n < N && m < M);
+            }
+        }
         __syncthreads();
 #pragma unroll
-        for (int q = 0; q < (PAIRS + WK - 1) / WK; ++q) {
+        for (int q = 0; q < MINE; ++q) {
             const int pr = q * WK + wk;
             if (PAIRS % WK != 0 && pr >= PAIRS) break;
             f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = {0.f, 0.f, 0.f, 0.f};
@@ -420,7 +472,7 @@ __global__ __launch_bounds__(TL::WM * TL::WN * TL::WK * 64, (TL::OCC * TL::WM * 
                 x += part[2 * pr * 64];
                 y += part[(2 * pr + 1) * 64];
             }
-            store_pair(pr / (NT / 2), pr % (NT / 2) * 2, x, y);
+            store_pair(pr / (NT / 2), pr % (NT / 2) * 2, x, y, bias[q], residual[q]);
         }
     }
 }
