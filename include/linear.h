@@ -29,9 +29,10 @@ enum { LINEAR_NONE = 0, LINEAR_RELU = 1, LINEAR_SILU = 2, LINEAR_GELU = 3, LINEA
 
 enum {
     LINEAR_OK = 0,
-    LINEAR_EINVAL = -1,       /* null, misaligned or overlapping pointer, bad size, stride, dtype or activation, no workspace */
+    LINEAR_EINVAL = -1,       /* null, misaligned or overlapping pointer, bad size, stride, dtype or activation */
     LINEAR_EUNSUPPORTED = -2, /* N, K or a stride beyond 2^22, M beyond 2^30, more tiles than a launch holds */
-    LINEAR_ELAUNCH = -3       /* the HIP runtime refused a launch */
+    LINEAR_ELAUNCH = -3,      /* the HIP runtime refused a launch */
+    LINEAR_ENOMEM = -4        /* gemm_linear_bwd without a workspace of the bytes that it needs; nothing has been enqueued */
 };
 
 /* A matrix: row r begins at data + r * stride (in elements), its columns lie on end.  data is aligned to 16 bytes, stride divides by 8 and is no
@@ -53,6 +54,13 @@ int gemm_linear(const linear_rows* x, const linear_rows* w, int w_rows_of_n, con
                 const linear_rows* pre, const linear_rows* out, int activation, int M, int N, int K, int dtype, void* workspace,
                 long long workspace_bytes, void* stream);
 
+/* The same for callers that take the memory call by call, with one look at the sizes: `scratch` is called at most once, with `owner` and the
+ * bytes, after the other arguments have been checked and only where there are any.  It returns memory as above or null (none), and must not throw. */
+typedef void* (*linear_scratch_fn)(void* owner, long long bytes);
+int gemm_linear_with(const linear_rows* x, const linear_rows* w, int w_rows_of_n, const void* bias, int bias_f32, const linear_rows* residual,
+                     const linear_rows* pre, const linear_rows* out, int activation, int M, int N, int K, int dtype, linear_scratch_fn scratch,
+                     void* owner, void* stream);
+
 /* Bytes that the sizes ask for (at most 64 MiB); negative: the error that the call would give. */
 long long gemm_linear_workspace(int M, int N, int K, int w_rows_of_n);
 
@@ -61,10 +69,14 @@ long long gemm_linear_workspace(int M, int N, int K, int w_rows_of_n);
  *  x   : needed for dw.  w: needed for dx.  dw has a layout of its own (dw_rows_of_n), as w has.
  *  dbias : fp32 [N], 16-byte aligned, written (not added to).
  *  dx, dw and dbias overlap nothing.
- *  workspace : gemm_linear_bwd_workspace bytes for the gradients that are given; null or fewer are refused unless it is 0. */
+ *  workspace : gemm_linear_bwd_workspace bytes for the gradients that are given; null or fewer are refused (LINEAR_ENOMEM) unless it is 0. */
 int gemm_linear_bwd(const linear_rows* dy, const linear_rows* x, const linear_rows* w, int w_rows_of_n, const linear_rows* pre,
                     const linear_rows* dx, const linear_rows* dw, int dw_rows_of_n, float* dbias, int activation, int M, int N, int K,
                     int dtype, void* workspace, long long workspace_bytes, void* stream);
+
+int gemm_linear_bwd_with(const linear_rows* dy, const linear_rows* x, const linear_rows* w, int w_rows_of_n, const linear_rows* pre,
+                         const linear_rows* dx, const linear_rows* dw, int dw_rows_of_n, float* dbias, int activation, int M, int N, int K,
+                         int dtype, linear_scratch_fn scratch, void* owner, void* stream);
 
 /* dx, dw, dbias: whether that gradient is asked for. */
 long long gemm_linear_bwd_workspace(int M, int N, int K, int w_rows_of_n, int dw_rows_of_n, int activation, int dx, int dw, int dbias);

@@ -126,8 +126,8 @@ def native():
                         for f in (L.kv4_append, L.kv4_read, L.kv4_attn, L.kv4_attn_workspace, L.qk_norm_rope, L.qk_norm_rope_bwd,
                                   L.qk_norm_rope_bwd_workspace)))
         n.bind_block(*(ctypes.cast(f, ctypes.c_void_p).value
-                       for f in (L.gemm_linear, L.gemm_linear_workspace, L.gemm_linear_bwd, L.gemm_linear_bwd_workspace, L.residual_norm,
-                                 L.residual_norm_bwd, L.residual_norm_bwd_workspace, L.qk_norm_rope_axes, L.qk_norm_rope_axes_bwd)))
+                       for f in (L.gemm_linear_with, L.gemm_linear_bwd_with, L.residual_norm, L.residual_norm_bwd, L.residual_norm_bwd_workspace,
+                                 L.qk_norm_rope_axes, L.qk_norm_rope_axes_bwd)))
         _native = n
     return _native
 

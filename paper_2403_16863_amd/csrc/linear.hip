@@ -49,17 +49,29 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a) {
     float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     if (n < a.N) {
         const uint16_t *dy = a.dy + n, *pre = a.pre + n;
-#pragma unroll 4
-        for (long long m = first + at; m < end; m += step) {
-            float g[8], v[8];
-            unpack8<T>(*(const u32x4*)(dy + m * a.lddy), g);
-            if (a.act) {
-                unpack8<T>(*(const u32x4*)(pre + m * a.ldpre), v);
-                act_slope8(v, g, a.act);
-                if (a.dz) *(u32x4*)(a.dz + m * a.N + n) = pack8<T>(g);
+        constexpr int AT_ONCE = 4;  // rows whose loads are in flight together
+        for (long long m0 = first + at; m0 < end; m0 += AT_ONCE * step) {
+            u32x4 gr[AT_ONCE], vr[AT_ONCE];
+#pragma unroll
+            for (int r = 0; r < AT_ONCE; ++r) {
+                const long long m = m0 + r * step;
+                gr[r] = vr[r] = u32x4{0, 0, 0, 0};
+                if (m < end) gr[r] = *(const u32x4*)(dy + m * a.lddy);
+                if (m < end && a.act) vr[r] = *(const u32x4*)(pre + m * a.ldpre);
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum[i] += g[i];
+            for (int r = 0; r < AT_ONCE; ++r) {
+                const long long m = m0 + r * step;
+                float g[8], v[8];
+                unpack8<T>(gr[r], g);
+                if (a.act) {
+                    unpack8<T>(vr[r], v);
+                    act_slope8(v, g, a.act);
+                    if (a.dz && m < end) *(u32x4*)(a.dz + m * a.N + n) = pack8<T>(g);
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum[i] += g[i];
+            }
         }
     }
     if (!a.sums) return;
@@ -92,22 +104,37 @@ __global__ __launch_bounds__(256) void bias_kernel(const float* sums, int chunks
 }
 
 // ---- choice of the tile.  With n tiles on the busiest of the 256 units, and f of the units' n rounds filled, a product takes about
-//     ceil(K / kstage) * max(ceil(n / occ) * alone, n * full) * (1 + load * f) + n * ends + 2.7     (us)
-// and in ranges of k a second launch and the parts' way through memory in addition.
+//     ceil(K / kstage) * max(ceil(n / occ) * alone, n * full) * (1 + load * f) * (1 + off_a) * (1 + off_b) * (1 + tokens) + n * ends + base + MB of C * out    (us)
+// (load: what the units take from each other; off_a, off_b: where rows of A, of B do not all begin on a line of 128 bytes; tokens: by rows of k, where A is read
+// by the transposing reads; ends: prologue and epilogue of a tile; out: the result's way to memory) and in ranges of k, whose MB of C are those of all parts in 32 bits,
+// a second launch and their reading in addition.  Fitted to the times of 9483 drawn products, M 1 .. 8192, N, K 8 .. 16384, in the three layouts, each on most tiles
+// and up to ten numbers of ranges, three sets of buffers in turn.  The standard deviation of time over model is 8 to 12 % by tile; what the model chooses
+// takes 2.4 % longer than the best that was measured (geometric mean; 14 % in the worst twentieth), with 64 x 64 tiles alone, which are the best for most, 12 %.
+// Each of the others is worth 0.05 to 0.6 % of that mean, and 10 to 15 % in its own range (779 x 1408 x 3904: 96 x 64 tiles on eight waves 17.6 us, the next best 21.0);
+// tiles of 64 x 128, 32 x 64 with k split four ways and 16 x 128 were built and gave nothing.
 struct Shape {
     int bm, bn, bk, wk, threads, occ;
-    float alone, full, load, ends;
+    float alone, full, load, ends, off_a, off_b, tokens, base, out;
 };
 template <int I>
-constexpr Shape shape(float alone, float full, float load, float ends) {
+constexpr Shape shape(float alone, float full, float load, float ends, float off_a, float off_b, float tokens, float base, float out) {
     using T = TileOf<I>;
-    return {T::BM, T::BN, T::BK, T::WK, T::WM * T::WN * T::WK * 64, T::OCC, alone, full, load, ends};
+    return {T::BM, T::BN, T::BK, T::WK, T::WM * T::WN * T::WK * 64, T::OCC, alone, full, load, ends, off_a, off_b, tokens, base, out};
 }
 static constexpr Shape kShapes[kTiles] = {
-    shape<0>(0.60f, 0.f, 0.3f, 0.5f),      shape<1>(0.229f, 0.288f, 0.06f, 0.11f), shape<2>(0.215f, 0.181f, 0.25f, 0.f),
-    shape<3>(0.310f, 0.f, 0.61f, 0.37f),   shape<4>(0.327f, 0.f, 0.62f, 1.02f),    shape<5>(0.579f, 0.395f, 0.39f, 0.41f),
-    shape<6>(0.443f, 0.f, 0.56f, 1.83f),   shape<7>(0.502f, 0.f, 0.80f, 2.39f),    shape<8>(0.768f, 0.f, 0.77f, 2.94f),
-    shape<9>(0.982f, 0.f, 0.66f, 4.20f)};
+    shape<0>(0.383f, 0.243f, 1.717f, 1.350f, 0.053f, 0.074f, 0.250f, 2.139f, 0.000f),
+    shape<1>(0.316f, 0.143f, 1.937f, 0.984f, 0.051f, 0.170f, 0.097f, 2.245f, 0.129f),
+    shape<2>(0.218f, 0.171f, 1.484f, 0.788f, 0.004f, 0.093f, 0.082f, 2.407f, 0.000f),
+    shape<3>(0.163f, 0.208f, 0.283f, 0.202f, 0.032f, 0.041f, -0.011f, 2.829f, 0.155f),
+    shape<4>(0.256f, 0.209f, 0.828f, 1.669f, 0.076f, 0.106f, 0.105f, 1.997f, 0.262f),
+    shape<5>(0.318f, 0.056f, 0.609f, 1.967f, 0.030f, 0.090f, 0.250f, 2.056f, 0.302f),
+    shape<6>(0.241f, 0.182f, 0.452f, 0.673f, 0.039f, 0.018f, 0.144f, 2.831f, 0.171f),
+    shape<7>(0.328f, 0.325f, 0.409f, 1.642f, 0.035f, -0.007f, 0.115f, 2.332f, 0.204f),
+    shape<8>(0.400f, 0.303f, 0.415f, 1.094f, 0.037f, -0.012f, 0.091f, 2.704f, 0.109f),
+    shape<9>(0.503f, 0.498f, 0.089f, 2.783f, 0.048f, -0.018f, 0.114f, 1.846f, 0.147f),
+    shape<10>(0.605f, 0.032f, 0.039f, 3.645f, 0.032f, -0.022f, 0.064f, 1.500f, 0.125f),
+    shape<11>(0.853f, 0.820f, 0.000f, 4.652f, 0.014f, -0.029f, 0.074f, 1.500f, 0.097f),
+    shape<12>(1.087f, 0.290f, 0.000f, 5.369f, 0.012f, -0.028f, 0.071f, 1.500f, 0.062f)};
 
 constexpr long long kUnits = 256, kPartBytes = 64ll << 20;
 constexpr int kMostRanges = 32;
@@ -128,26 +155,30 @@ static Plan plan_of(int tile, int M, int N, int K, int ranges) {
     return {tile, ranges, kc, ranges > 1 ? 4ll * ranges * M * N : 0};
 }
 
-static float time_of(const Shape& s, int M, int N, int K, int ranges, int kc) {
-    const long long tiles = tiles_of(s, M, N) * ranges, n = (tiles + kUnits - 1) / kUnits;
-    const long long stages = ((long long)(ranges > 1 ? kc : K) + s.bk * s.wk - 1) / (s.bk * s.wk);
-    const float alone = (float)((n + s.occ - 1) / s.occ) * s.alone, full = (float)n * s.full, filled = (float)tiles / (float)(n * kUnits);
-    const float us = (float)stages * (alone > full ? alone : full) * (1.f + s.load * filled) + (float)n * s.ends + 2.7f;
-    return ranges > 1 ? us + 2.3f + 0.4e-6f * 4.f * (float)ranges * (float)M * (float)N : us;
+static float time_of(const Shape& s, long long tiles, int M, int N, const Plan& p, int K, float factor) {
+    const bool parts = p.ranges > 1;
+    tiles *= p.ranges;
+    const int n = (int)((tiles + kUnits - 1) / kUnits), stages = (int)(((parts ? p.kc : K) + s.bk * s.wk - 1) / (s.bk * s.wk));
+    const float alone = (float)((n + s.occ - 1) / s.occ) * s.alone, full = (float)n * s.full, filled = (float)tiles / ((float)n * kUnits);
+    const float us = (float)stages * (alone > full ? alone : full) * (1.f + s.load * filled) * factor + (float)n * s.ends + s.base;
+    const float mb = 1e-6f * (float)M * (float)N;
+    return parts ? us + 2.10f + 4.f * (float)p.ranges * mb * (0.55f + s.out) : us + 2.f * mb * s.out;
 }
 
 static Plan choose(int M, int N, int K, int layout, bool memory) {
     Plan best = {-1, 1, K, 0};
     float best_us = 0;
+    const bool off_a = (layout == TOKENS ? M : K) % 64, off_b = (layout == ROWS_N ? K : N) % 64;
     for (int t = 0; t < kTiles; ++t) {
         const Shape& s = kShapes[t];
         if (!fits(s, M, N, 1)) continue;
         const long long tiles = tiles_of(s, M, N);
-        for (int r = 1; r <= kMostRanges; ++r) {
-            if (r > 1 && (!memory || tiles * r > kUnits * s.occ || (long long)r * 256 > K)) break;
-            const Plan p = plan_of(t, M, N, K, r);
+        const float factor = (off_a ? 1.f + s.off_a : 1.f) * (off_b ? 1.f + s.off_b : 1.f) * (layout == TOKENS ? 1.f + s.tokens : 1.f);
+        for (int r : {1, 2, 3, 4, 6, 8, 12, 16, 24, kMostRanges}) {
+            if (r > 1 && (!memory || tiles * r > kUnits * s.occ || (long long)r * 128 > K)) break;
+            const Plan p = r > 1 ? plan_of(t, M, N, K, r) : Plan{t, 1, K, 0};
             if (p.ranges != r || p.bytes > kPartBytes) continue;
-            const float us = time_of(s, M, N, K, r, p.kc);
+            const float us = time_of(s, tiles, M, N, p, K, factor);
             if (best.tile < 0 || us < best_us) best = p, best_us = us;
         }
     }
@@ -205,6 +236,15 @@ static int stride_of(const linear_rows* t, int rows, int columns) { return rows 
 static Rows2D block(const linear_rows* t, int rows, int columns) { return {given(t) ? t->data : nullptr, rows, columns, given(t) ? t->stride : 0}; }
 static Rows2D vector_of(const void* p, long long bytes) { return {p, 1, bytes / 2, 0}; }
 
+// Scratch memory of a call: the caller's, or asked for by the call once it knows how much.
+struct Memory {
+    void* given;
+    long long bytes;
+    linear_scratch_fn ask;
+    void* owner;
+    void* take(long long need) const { return ask ? ask(owner, need) : bytes >= need ? given : nullptr; }
+};
+
 static long long up(long long bytes) { return (bytes + 255) / 256 * 256; }
 
 // Workgroups of the activation's backward step: 1024 where there are rows enough for them to have two passes each.
@@ -245,21 +285,8 @@ static Backward backward_of(int M, int N, int K, int w_rows_of_n, int dw_rows_of
     return b;
 }
 
-}  // namespace linear
-
-extern "C" {
-
-long long gemm_linear_workspace(int M, int N, int K, int w_rows_of_n) {
-    using namespace linear;
-    if (const int rc = check_sizes(M, N, K, LINEAR_F16, LINEAR_NONE)) return rc;
-    const Plan p = choose(M, N, K, w_rows_of_n ? ROWS_N : ROWS, true);
-    return p.tile < 0 ? LINEAR_EUNSUPPORTED : p.bytes;
-}
-
-int gemm_linear(const linear_rows* x, const linear_rows* w, int w_rows_of_n, const void* bias, int bias_f32, const linear_rows* residual,
-                const linear_rows* pre, const linear_rows* out, int activation, int M, int N, int K, int dtype, void* workspace,
-                long long workspace_bytes, void* stream) {
-    using namespace linear;
+static int forward(const linear_rows* x, const linear_rows* w, int w_rows_of_n, const void* bias, int bias_f32, const linear_rows* residual,
+                   const linear_rows* pre, const linear_rows* out, int activation, int M, int N, int K, int dtype, const Memory& memory, void* stream) {
     if (const int rc = check_sizes(M, N, K, dtype, activation)) return rc;
     const int wr = w_rows_of_n ? N : K, wc = w_rows_of_n ? K : N;
     if (const int rc = check_matrix(x, M, K)) return rc;
@@ -269,7 +296,7 @@ int gemm_linear(const linear_rows* x, const linear_rows* w, int w_rows_of_n, con
         if (const int rc = check_matrix(residual, M, N)) return rc;
     if (given(pre))
         if (const int rc = check_matrix(pre, M, N)) return rc;
-    if ((uintptr_t)bias % 16 || (uintptr_t)workspace % 16) return LINEAR_EINVAL;
+    if ((uintptr_t)bias % 16 || (uintptr_t)memory.given % 16) return LINEAR_EINVAL;
     const Rows2D xs = block(x, M, K), ws = block(w, wr, wc), bs = vector_of(bias, (long long)N * (bias_f32 ? 4 : 2)), rs = block(residual, M, N);
     const Rows2D os = block(out, M, N), ps = block(pre, M, N);
     const bool in_place = given(residual) && residual->data == out->data && (M == 1 || residual->stride == out->stride);
@@ -278,8 +305,9 @@ int gemm_linear(const linear_rows* x, const linear_rows* w, int w_rows_of_n, con
     const int layout = w_rows_of_n ? ROWS_N : ROWS;
     Plan plan = choose(M, N, K, layout, true);
     if (plan.tile < 0) return LINEAR_EUNSUPPORTED;
+    void* const workspace = plan.bytes ? memory.take(plan.bytes) : nullptr;
     if (plan.bytes) {
-        if (!workspace || workspace_bytes < plan.bytes) {
+        if (!workspace) {
             plan = choose(M, N, K, layout, false);
         } else {
             const Rows2D mine = vector_of(workspace, plan.bytes);
@@ -296,18 +324,9 @@ int gemm_linear(const linear_rows* x, const linear_rows* w, int w_rows_of_n, con
     return run(plan, layout, dtype, a, workspace, stream);
 }
 
-long long gemm_linear_bwd_workspace(int M, int N, int K, int w_rows_of_n, int dw_rows_of_n, int activation, int dx, int dw, int dbias) {
-    using namespace linear;
-    if (const int rc = check_sizes(M, N, K, LINEAR_F16, activation)) return rc;
-    if (!dx && !dw && !dbias) return LINEAR_EINVAL;
-    const Backward b = backward_of(M, N, K, w_rows_of_n, dw_rows_of_n, activation, dx, dw, dbias);
-    return b.dx.tile < 0 || b.dw.tile < 0 ? LINEAR_EUNSUPPORTED : b.total();
-}
-
-int gemm_linear_bwd(const linear_rows* dy, const linear_rows* x, const linear_rows* w, int w_rows_of_n, const linear_rows* pre,
+static int backward(const linear_rows* dy, const linear_rows* x, const linear_rows* w, int w_rows_of_n, const linear_rows* pre,
                     const linear_rows* dx, const linear_rows* dw, int dw_rows_of_n, float* dbias, int activation, int M, int N, int K,
-                    int dtype, void* workspace, long long workspace_bytes, void* stream) {
-    using namespace linear;
+                    int dtype, const Memory& memory, void* stream) {
     if (const int rc = check_sizes(M, N, K, dtype, activation)) return rc;
     const bool want_x = given(dx), want_w = given(dw);
     if (!want_x && !want_w && !dbias) return LINEAR_EINVAL;
@@ -323,11 +342,12 @@ int gemm_linear_bwd(const linear_rows* dy, const linear_rows* x, const linear_ro
         if (const int rc = check_matrix(x, M, K)) return rc;
         if (const int rc = check_matrix(dw, dwr, dwc)) return rc;
     }
-    if ((uintptr_t)dbias % 16 || (uintptr_t)workspace % 16) return LINEAR_EINVAL;
+    if ((uintptr_t)dbias % 16 || (uintptr_t)memory.given % 16) return LINEAR_EINVAL;
     const Backward b = backward_of(M, N, K, w_rows_of_n, dw_rows_of_n, activation, want_x, want_w, dbias);
     if (b.dx.tile < 0 || b.dw.tile < 0 || (long long)b.slope.blocks * b.slope.chunks * 256 > (long long)UINT_MAX || b.slope.chunks > 65535)
         return LINEAR_EUNSUPPORTED;
-    if (b.total() && (!workspace || workspace_bytes < b.total())) return LINEAR_EINVAL;
+    void* const workspace = b.total() ? memory.take(b.total()) : nullptr;
+    if (b.total() && !workspace) return LINEAR_ENOMEM;
     const Rows2D in[] = {block(dy, M, N), activation ? block(pre, M, N) : Rows2D{}, want_w ? block(x, M, K) : Rows2D{},
                          want_x ? block(w, wr, wc) : Rows2D{}};
     const Rows2D out[] = {want_x ? block(dx, M, K) : Rows2D{}, want_w ? block(dw, dwr, dwc) : Rows2D{}, vector_of(dbias, 4ll * N),
@@ -376,6 +396,51 @@ int gemm_linear_bwd(const linear_rows* dy, const linear_rows* x, const linear_ro
     return LINEAR_OK;
 }
 
+}  // namespace linear
+
+extern "C" {
+
+long long gemm_linear_workspace(int M, int N, int K, int w_rows_of_n) {
+    using namespace linear;
+    if (const int rc = check_sizes(M, N, K, LINEAR_F16, LINEAR_NONE)) return rc;
+    const Plan p = choose(M, N, K, w_rows_of_n ? ROWS_N : ROWS, true);
+    return p.tile < 0 ? LINEAR_EUNSUPPORTED : p.bytes;
+}
+
+int gemm_linear(const linear_rows* x, const linear_rows* w, int w_rows_of_n, const void* bias, int bias_f32, const linear_rows* residual,
+                const linear_rows* pre, const linear_rows* out, int activation, int M, int N, int K, int dtype, void* workspace,
+                long long workspace_bytes, void* stream) {
+    return linear::forward(x, w, w_rows_of_n, bias, bias_f32, residual, pre, out, activation, M, N, K, dtype, {workspace, workspace_bytes, nullptr, nullptr},
+                           stream);
+}
+
+int gemm_linear_with(const linear_rows* x, const linear_rows* w, int w_rows_of_n, const void* bias, int bias_f32, const linear_rows* residual,
+                     const linear_rows* pre, const linear_rows* out, int activation, int M, int N, int K, int dtype, linear_scratch_fn scratch,
+                     void* owner, void* stream) {
+    return linear::forward(x, w, w_rows_of_n, bias, bias_f32, residual, pre, out, activation, M, N, K, dtype, {nullptr, 0, scratch, owner}, stream);
+}
+
+long long gemm_linear_bwd_workspace(int M, int N, int K, int w_rows_of_n, int dw_rows_of_n, int activation, int dx, int dw, int dbias) {
+    using namespace linear;
+    if (const int rc = check_sizes(M, N, K, LINEAR_F16, activation)) return rc;
+    if (!dx && !dw && !dbias) return LINEAR_EINVAL;
+    const Backward b = backward_of(M, N, K, w_rows_of_n, dw_rows_of_n, activation, dx, dw, dbias);
+    return b.dx.tile < 0 || b.dw.tile < 0 ? LINEAR_EUNSUPPORTED : b.total();
+}
+
+int gemm_linear_bwd(const linear_rows* dy, const linear_rows* x, const linear_rows* w, int w_rows_of_n, const linear_rows* pre,
+                    const linear_rows* dx, const linear_rows* dw, int dw_rows_of_n, float* dbias, int activation, int M, int N, int K,
+                    int dtype, void* workspace, long long workspace_bytes, void* stream) {
+    return linear::backward(dy, x, w, w_rows_of_n, pre, dx, dw, dw_rows_of_n, dbias, activation, M, N, K, dtype,
+                            {workspace, workspace_bytes, nullptr, nullptr}, stream);
+}
+
+int gemm_linear_bwd_with(const linear_rows* dy, const linear_rows* x, const linear_rows* w, int w_rows_of_n, const linear_rows* pre,
+                         const linear_rows* dx, const linear_rows* dw, int dw_rows_of_n, float* dbias, int activation, int M, int N, int K,
+                         int dtype, linear_scratch_fn scratch, void* owner, void* stream) {
+    return linear::backward(dy, x, w, w_rows_of_n, pre, dx, dw, dw_rows_of_n, dbias, activation, M, N, K, dtype, {nullptr, 0, scratch, owner}, stream);
+}
+
 int linear_num_tiles(void) { return linear::kTiles; }
 
 int linear_choice(int M, int N, int K, int layout, int* tile, int* ranges) {
@@ -417,6 +482,7 @@ const char* linear_strerror(int code) {
         case LINEAR_OK: return "ok";
         case LINEAR_EINVAL: return "invalid argument";
         case LINEAR_EUNSUPPORTED: return "unsupported size";
+        case LINEAR_ENOMEM: return "no workspace, or too small a one";
         case LINEAR_ELAUNCH: return "the HIP runtime refused the launch";
         default: return "unknown error";
     }

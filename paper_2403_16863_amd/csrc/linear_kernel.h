@@ -202,7 +202,7 @@ struct Piece {
     static __device__ __forceinline__ int code(int row) {
         if (ALONG) return gemm::a_code<CHUNKS>(row);
         const int hi = (row >> 3) & 1;
-        return SLOTS % 8 == 0 ? ((row & 3) | (hi << 2)) : SLOTS % 4 == 0 ? (((row >> 1) & 1) | (hi << 1)) : SLOTS == 2 ? hi : 0;
+        return SLOTS % 8 == 0 ? ((row & 3) | (hi << 2)) : SLOTS % 4 == 0 ? (((row >> 1) & 1) | (hi << 1)) : SLOTS % 2 == 0 ? hi : 0;
     }
     unsigned voff[LOADS];
     int k[LOADS];       // k of the lane's chunk inside a stage

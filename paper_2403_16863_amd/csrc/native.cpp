@@ -42,10 +42,8 @@ decltype(&qk_norm_rope_bwd) g_rope_bwd = nullptr;
 decltype(&qk_norm_rope_bwd_workspace) g_rope_bwd_workspace = nullptr;
 decltype(&qk_norm_rope_axes) g_rope_axes = nullptr;
 decltype(&qk_norm_rope_axes_bwd) g_rope_axes_bwd = nullptr;
-decltype(&gemm_linear) g_linear = nullptr;
-decltype(&gemm_linear_workspace) g_linear_workspace = nullptr;
-decltype(&gemm_linear_bwd) g_linear_bwd = nullptr;
-decltype(&gemm_linear_bwd_workspace) g_linear_bwd_workspace = nullptr;
+decltype(&gemm_linear_with) g_linear = nullptr;
+decltype(&gemm_linear_bwd_with) g_linear_bwd = nullptr;
 decltype(&residual_norm) g_norm = nullptr;
 decltype(&residual_norm_bwd) g_norm_bwd = nullptr;
 decltype(&residual_norm_bwd_workspace) g_norm_bwd_workspace = nullptr;
@@ -523,15 +521,12 @@ PyObject* linear(PyObject* const* args, Py_ssize_t nargs) {
         return not_plain();
     void* stream;
     if (!stream_of(args[8], THPVariable_Unpack(args[0]), &stream)) return not_plain();
-    const long long need = g_linear_workspace(M, N, K, rows_of_n);
-    if (need < 0) return PyLong_FromLong(need);
     int rc;
     Py_BEGIN_ALLOW_THREADS
     {
         Workspace own(stream, r.device, true);
-        void* ws = need ? own.take(need) : nullptr;
         rc = g_linear(&x, &w, rows_of_n, bias ? bias->data_ptr() : nullptr, bias && bias->scalar_type() == at::kFloat, &residual, &pre, &out, act, M, N, K, dt,
-                      ws, ws ? need : 0, stream);
+                      &Workspace::take, &own, stream);
     }
     Py_END_ALLOW_THREADS
     return PyLong_FromLong(rc);
@@ -554,18 +549,15 @@ PyObject* linear_bwd(PyObject* const* args, Py_ssize_t nargs) {
     void* stream;
     if (!stream_of(args[9], THPVariable_Unpack(args[0]), &stream)) return not_plain();
     if (!K) K = 8;  // (dbias alone: no product)
-    const long long need = g_linear_bwd_workspace(M, N, K, w_rows_of_n, dw_rows_of_n, act, want_x, want_w, dbias != nullptr);
-    if (need < 0) return PyLong_FromLong(need);
-    long rc = kNotPlain;
+    long rc;
     float* const db = (float*)data(dbias);
     Py_BEGIN_ALLOW_THREADS
     {
         Workspace own(stream, r.device, true);
-        void* ws = need ? own.take(need) : nullptr;
-        if (ws || !need) rc = g_linear_bwd(&dy, &x, &w, w_rows_of_n, &pre, &dx, &dw, dw_rows_of_n, db, act, M, N, K, dt, ws, need, stream);
+        rc = g_linear_bwd(&dy, &x, &w, w_rows_of_n, &pre, &dx, &dw, dw_rows_of_n, db, act, M, N, K, dt, &Workspace::take, &own, stream);
     }
     Py_END_ALLOW_THREADS
-    return PyLong_FromLong(rc);
+    return rc == LINEAR_ENOMEM ? not_plain() : PyLong_FromLong(rc);  // (no memory of torch's: Python says why)
 }
 
 // Norms with the residual stream: tensors [B, N, C] of one type and size.
@@ -678,15 +670,14 @@ PyObject* bind_cached(PyObject*, PyObject* args) {
     Py_RETURN_NONE;
 }
 
-// bind_block(addresses of gemm_linear, gemm_linear_workspace, gemm_linear_bwd, gemm_linear_bwd_workspace, residual_norm, residual_norm_bwd,
-// residual_norm_bwd_workspace, qk_norm_rope_axes and qk_norm_rope_axes_bwd)
+// bind_block(addresses of gemm_linear_with, gemm_linear_bwd_with, residual_norm, residual_norm_bwd, residual_norm_bwd_workspace, qk_norm_rope_axes and
+// qk_norm_rope_axes_bwd)
 PyObject* bind_block(PyObject*, PyObject* args) {
-    unsigned long long f[9];
-    if (!PyArg_ParseTuple(args, "KKKKKKKKK", &f[0], &f[1], &f[2], &f[3], &f[4], &f[5], &f[6], &f[7], &f[8])) return nullptr;
-    g_rope_axes = (decltype(g_rope_axes))f[7], g_rope_axes_bwd = (decltype(g_rope_axes_bwd))f[8];
-    g_linear = (decltype(g_linear))f[0], g_linear_workspace = (decltype(g_linear_workspace))f[1];
-    g_linear_bwd = (decltype(g_linear_bwd))f[2], g_linear_bwd_workspace = (decltype(g_linear_bwd_workspace))f[3];
-    g_norm = (decltype(g_norm))f[4], g_norm_bwd = (decltype(g_norm_bwd))f[5], g_norm_bwd_workspace = (decltype(g_norm_bwd_workspace))f[6];
+    unsigned long long f[7];
+    if (!PyArg_ParseTuple(args, "KKKKKKK", &f[0], &f[1], &f[2], &f[3], &f[4], &f[5], &f[6])) return nullptr;
+    g_linear = (decltype(g_linear))f[0], g_linear_bwd = (decltype(g_linear_bwd))f[1];
+    g_norm = (decltype(g_norm))f[2], g_norm_bwd = (decltype(g_norm_bwd))f[3], g_norm_bwd_workspace = (decltype(g_norm_bwd_workspace))f[4];
+    g_rope_axes = (decltype(g_rope_axes))f[5], g_rope_axes_bwd = (decltype(g_rope_axes_bwd))f[6];
     Py_RETURN_NONE;
 }
 

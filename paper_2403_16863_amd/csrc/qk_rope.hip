@@ -71,28 +71,38 @@ __device__ __forceinline__ float vector_sum(float x) {
     return x;
 }
 
-// The cosines and sines of a lane's 8 pairs by several axes, `mine` its word of AxesArgs::axis.  Axes mostly begin and end between lanes, and then a lane
-// reads one row of the tables; one whose pairs have several axes reads a row for each and takes its pairs from it.
+// The cosines and sines of a lane's 8 pairs by several axes, `mine` its word of AxesArgs::axis.  Axes mostly begin and end between lanes, or once inside one: a
+// lane asks for the rows of its first and its last pair's axes at once, and only one with a third (axes that take turns) for more behind them.
 template <int D>
 __device__ __forceinline__ void angles_by_axes(const float* cos, const float* sin, const int* positions, int rows, int axes, unsigned mine, int l, float* c, float* s) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) c[i] = 1, s[i] = 0;
-    for (int axis = 0; axis < axes; ++axis) {
-        unsigned other = mine ^ axis * 0x11111111u;  // nibbles of 0: this axis's pairs
-        other = (other | other >> 1 | other >> 2 | other >> 3) & 0x11111111u;
-        if (other == 0x11111111u) continue;
-        const int at = positions[axis];
-        float x[8], y[8];
-        if ((unsigned)at < (unsigned)rows) {
+    auto row = [&](unsigned axis, float* x, float* y) __attribute__((always_inline)) {
+        const int at = axis == kNoAxis ? 0 : positions[axis];
+        const float none = axis == kNoAxis ? 1.f : __uint_as_float(0x7fc00000u);
+        if (axis != kNoAxis && (unsigned)at < (unsigned)rows) {
             load8f(cos + (long long)at * (D / 2) + 8 * l, x);
             load8f(sin + (long long)at * (D / 2) + 8 * l, y);
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = y[i] = __uint_as_float(0x7fc00000u);
+            for (int i = 0; i < 8; ++i) x[i] = none, y[i] = axis == kNoAxis ? 0.f : none;
         }
+    };
+    const unsigned first = mine & 15, last = mine >> 28;
+    float x[8], y[8];
+    row(first, c, s);
+    if (mine == first * 0x11111111u) return;
+    row(last, x, y);
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (!(other >> 4 * i & 1)) c[i] = x[i], s[i] = y[i];
+    for (int i = 0; i < 8; ++i)
+        if ((mine >> 4 * i & 15) == last) c[i] = x[i], s[i] = y[i];
+    for (unsigned axis = 0; axis <= kNoAxis; axis = axis + 1 == (unsigned)axes ? kNoAxis : axis + 1) {
+        unsigned other = mine ^ axis * 0x11111111u;  // nibbles of 0: this axis's pairs
+        other = (other | other >> 1 | other >> 2 | other >> 3) & 0x11111111u;
+        if (other != 0x11111111u && axis != first && axis != last) {
+            row(axis, x, y);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (!(other >> 4 * i & 1)) c[i] = x[i], s[i] = y[i];
+        }
     }
 }
 

@@ -524,7 +524,7 @@ static int launch(const void* fn, dim3 grid, int threads, void* args, void* stre
 }
 
 // Units of a backward pass: two workgroups of four waves to a unit of the card are enough to keep its memory busy, and no more, for each has sums to
-// be added; a unit has 8 rounds of tokens at least, where there are as many.
+// be added.
 struct Units {
     int runs, length, chunks, rows, blocks;
 };
@@ -535,7 +535,7 @@ static Units units_of(int B, int N, int C, bool sequences) {
     u.runs = sequences ? B : 1;
     u.length = sequences ? N : B * N;
     const int limit = k.waves > 4 ? 256 : 512, each = u.runs >= limit ? 1 : limit / u.runs;
-    const long long most = ((long long)u.length + 8 * groups - 1) / (8 * groups), chunks = each < most ? each : most;
+    const long long most = ((long long)u.length + groups - 1) / groups, chunks = each < most ? each : most;
     u.rows = (int)((u.length + chunks - 1) / chunks + groups - 1) / groups * groups;
     u.chunks = (int)(((long long)u.length + u.rows - 1) / u.rows);
     const long long units = (long long)u.runs * u.chunks;

@@ -11,13 +11,15 @@ import ctypes
 from . import binding
 
 LINEAR_F16, LINEAR_BF16 = 0, 1
-LINEAR_OK, LINEAR_EINVAL, LINEAR_EUNSUPPORTED, LINEAR_ELAUNCH = 0, -1, -2, -3
+LINEAR_OK, LINEAR_EINVAL, LINEAR_EUNSUPPORTED, LINEAR_ELAUNCH, LINEAR_ENOMEM = 0, -1, -2, -3, -4
 ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}
 ROWS, ROWS_N, TOKENS = 0, 1, 2      # layouts of linear_product
 
 # every symbol include/linear.h declares
-SYMBOLS = ("gemm_linear", "gemm_linear_workspace", "gemm_linear_bwd", "gemm_linear_bwd_workspace", "linear_product", "linear_num_tiles",
-           "linear_choice", "linear_strerror")
+SYMBOLS = ("gemm_linear", "gemm_linear_with", "gemm_linear_workspace", "gemm_linear_bwd", "gemm_linear_bwd_with", "gemm_linear_bwd_workspace",
+           "linear_product", "linear_num_tiles", "linear_choice", "linear_strerror")
+
+SCRATCH_FN = ctypes.CFUNCTYPE(ctypes.c_void_p, ctypes.c_void_p, ctypes.c_longlong)  # linear_scratch_fn
 
 
 class Rows(ctypes.Structure):  # linear_rows
@@ -34,6 +36,10 @@ def lib():
         vp, i, ll, r, ip = ctypes.c_void_p, ctypes.c_int, ctypes.c_longlong, ctypes.POINTER(Rows), ctypes.POINTER(ctypes.c_int)
         L.gemm_linear.restype = i
         L.gemm_linear.argtypes = [r, r, i, vp, i, r, r, r, i, i, i, i, i, vp, ll, vp]
+        L.gemm_linear_with.restype = i
+        L.gemm_linear_with.argtypes = [r, r, i, vp, i, r, r, r, i, i, i, i, i, SCRATCH_FN, vp, vp]
+        L.gemm_linear_bwd_with.restype = i
+        L.gemm_linear_bwd_with.argtypes = [r, r, r, i, r, r, r, i, vp, i, i, i, i, i, SCRATCH_FN, vp, vp]
         L.gemm_linear_workspace.restype = ll
         L.gemm_linear_workspace.argtypes = [i] * 4
         L.gemm_linear_bwd.restype = i

@@ -73,7 +73,9 @@ def test_forward_and_backward_match_the_formulas(d, sections, alternating, inter
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("d", [64, 128])
 def test_equal_positions_are_the_rotation_by_one(d, dtype):
-    """With the same position on every axis the result is qk_norm_rope's, bit for bit, and so is one axis."""
+    """With the same position on every axis the result is qk_norm_rope's, and so is one axis.  Not bit for bit: of the two products of a pair's channel, a c - b s,
+    one is fused with the sum, and which is each kernel's own compilation's choice, so that the sums in 32 bits may differ by 2^-24 (|a c| + |b s|) and a rounding of
+    their own, below 2^-22 (|a| + |b|), and their roundings to 16 bits by a step then."""
     from paper_2403_16863_amd import rope
     q, k, dqo, dko, (qw, kw), c, s, positions = inputs(2, 33, 4, 2, d, 1, dtype, dtype)
     one = [torch.empty(2, 33, n, d, dtype=dtype, device="cuda") for n in (4, 2, 4, 2)]
@@ -87,7 +89,13 @@ def test_equal_positions_are_the_rotation_by_one(d, dtype):
         two = [torch.empty_like(t) for t in one]
         rope.qk_norm_rope_axes(q, k, two[0], two[1], c, s, p, axes, qw, kw)
         rope.qk_norm_rope_axes_bwd(dqo, dko, q, k, two[2], two[3], c, s, p, axes, qw, kw, *weights[2:])
-        assert all(same(a, b) for a, b in zip(one, two)) and same(weights[0], weights[2]) and same(weights[1], weights[3])
+        for a, b in zip(one, two):
+            size = a.float().abs().amax(-1, keepdim=True)              # a pair's channels are d/2 apart: the token's largest bounds both
+            assert ((a.float() - b.float()).abs() <= 2 * U[dtype] * a.float().abs() + 2.0 ** -19 * size).all()
+        for a, b, x, dy in ((weights[0], weights[2], q, dqo), (weights[1], weights[3], k, dko)):
+            # terms g n with |g| <= 2 |dy| and |n| <= |x| / rms(x), each g off by 2^-22 of its pair
+            n = x.float() * torch.rsqrt(x.float().square().mean(-1, keepdim=True))
+            assert ((a - b).abs() <= 2.0 ** -20 * 2 * dy.float().abs().max() * n.abs().sum((0, 1, 2)).max()).all()
 
 
 def test_positions_outside_the_table_touch_their_own_pairs():

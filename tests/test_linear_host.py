@@ -26,7 +26,7 @@ def test_every_declared_symbol_is_exported_and_bound():
     names = sorted(set(re.findall(r"\b((?:gemm_)?linear[a-z_0-9]*)\s*\(", text)))
     assert names == sorted(linear.SYMBOLS)
     for n in names:
-        assert hasattr(linear.lib(), n) and hasattr(linear, n)
+        assert hasattr(linear.lib(), n) and (hasattr(linear, n) or n.endswith("_with"))     # (those are the native call path's)
 
 
 # 5 rows of 64 columns (x: 5 x 64, w: 64 x 32 or 32 x 64), rows of 128 bytes
@@ -72,15 +72,38 @@ def test_what_is_not_refused():
 
 
 def test_backward_refuses_bad_arguments():
-    for bad in (dict(dx=NONE, dw=NONE, dbias=0), dict(dy=NONE), dict(w=NONE), dict(x=NONE), dict(pre=NONE), dict(dbias=0x70008), dict(ws=0x100008), dict(ws=0),
-                dict(bytes_=0), dict(bytes_=16), dict(act=9), dict(M=0), dict(N=4), dict(K=4), dict(dt=3), dict(dw=m(0x60000, 24)), dict(dw_rows_of_n=1),
+    for bad in (dict(dx=NONE, dw=NONE, dbias=0), dict(dy=NONE), dict(w=NONE), dict(x=NONE), dict(pre=NONE), dict(dbias=0x70008), dict(ws=0x100008), dict(act=9), dict(M=0), dict(N=4), dict(K=4), dict(dt=3), dict(dw=m(0x60000, 24)), dict(dw_rows_of_n=1),
                 dict(dx=m(0x50008)), dict(dy=m(0x10000, 24))):
         assert backward(**bad) == linear.LINEAR_EINVAL, bad
+    for bad in (dict(ws=0), dict(bytes_=0), dict(bytes_=16)):
+        assert backward(**bad) == linear.LINEAR_ENOMEM, bad
     for bad in (dict(dx=m(0x10000)), dict(dx=m(0x20000)), dict(dx=m(0x60000)), dict(dw=m(0x20000, 32)), dict(dw=m(0x40000, 32)), dict(dbias=0x60000),
                 dict(dbias=0x10000), dict(ws=0x50000 - 256), dict(ws=0x30000)):
         assert backward(**bad) == linear.LINEAR_EINVAL, bad
     for bad in (dict(M=(1 << 30) + 1), dict(N=(1 << 22) + 8), dict(K=(1 << 22) + 8)):
         assert backward(**bad) == linear.LINEAR_EUNSUPPORTED, bad
+
+
+def test_memory_asked_for_by_the_call():
+    """Once, with the bytes of the workspace functions, and none without a use for it."""
+    if not ON_CPU:
+        pytest.skip("the addresses are nobody's")
+    asked = []
+
+    def scratch(owner, n):
+        asked.append((owner, n))
+        return None
+    fn, L = linear.SCRATCH_FN(scratch), linear.lib()
+    M, N, K = 4, 64, 16384
+    args = (m(0x1000000, K), m(0x2000000, N), 0, None, 0, NONE, NONE, m(0x3000000, N), 0, M, N, K, 0, fn, p(7), None)
+    rc = L.gemm_linear_with(*args)
+    assert asked == [(7, linear.gemm_linear_workspace(M, N, K))] and rc == linear.LINEAR_ELAUNCH
+    asked.clear()
+    back = (m(0x1000000, N), m(0x2000000, K), m(0x3000000, N), 0, m(0x4000000, N), m(0x5000000, K), m(0x6000000, N), 0, None, 1, M, N, K, 0, fn, None, None)
+    assert L.gemm_linear_bwd_with(*back) == linear.LINEAR_ENOMEM
+    assert asked == [(None, linear.gemm_linear_bwd_workspace(M, N, K, "relu", dbias=False))]
+    asked.clear()
+    assert L.gemm_linear_with(NONE, *args[1:]) == linear.LINEAR_EINVAL and L.gemm_linear_bwd_with(NONE, *back[1:]) == linear.LINEAR_EINVAL and not asked
 
 
 def test_products_refuse_bad_arguments():
