@@ -49,7 +49,7 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a) {
     float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     if (n < a.N) {
         const uint16_t *dy = a.dy + n, *pre = a.pre + n;
-        constexpr int AT_ONCE = 4;  // rows whose loads are in flight together
+        constexpr int AT_ONCE = 2;  // rows whose loads are in flight together
         for (long long m0 = first + at; m0 < end; m0 += AT_ONCE * step) {
             u32x4 gr[AT_ONCE], vr[AT_ONCE];
 #pragma unroll
@@ -86,21 +86,22 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a) {
     }
 }
 
-// dbias from the chunks' sums: 32 columns a workgroup, 8 threads to a column.
-__global__ __launch_bounds__(256) void bias_kernel(const float* sums, int chunks, int N, float* dbias) {
-    __shared__ float part[256];
+// dbias from the chunks' sums: 32 columns a workgroup, 32 threads to a column, so that 128 chunks are four loads to a thread.
+__global__ __launch_bounds__(1024) void bias_kernel(const float* sums, int chunks, int N, float* dbias) {
+    __shared__ float part[1024];
     const int c = blockIdx.x * 32 + threadIdx.x % 32;
     float t = 0;
     if (c < N) {
-#pragma unroll 8
-        for (int i = threadIdx.x / 32; i < chunks; i += 8) t += sums[(size_t)i * N + c];
+#pragma unroll 4
+        for (int i = threadIdx.x / 32; i < chunks; i += 32) t += sums[(size_t)i * N + c];
     }
     part[threadIdx.x] = t;
-    __syncthreads();
-    if (threadIdx.x >= 32 || c >= N) return;
 #pragma unroll
-    for (int i = 1; i < 8; ++i) t += part[threadIdx.x + 32 * i];
-    dbias[c] = t;
+    for (int n = 512; n >= 32; n /= 2) {
+        __syncthreads();
+        if (threadIdx.x < n) part[threadIdx.x] += part[threadIdx.x + n];
+    }
+    if (threadIdx.x < 32 && c < N) dbias[c] = part[threadIdx.x];
 }
 
 // ---- choice of the tile.  With n tiles on the busiest of the 256 units, and f of the units' n rounds filled, a product takes about
@@ -259,7 +260,8 @@ static SlopeGrid slope_grid(int M, int N) {
     const int pass = 256 / g.lanes;
     const long long most = (M + 2ll * pass - 1) / (2 * pass), want = g.blocks >= 1024 ? 1 : 1024 / g.blocks;
     const long long chunks = want < most ? want : most;
-    g.rows = (int)(((M + chunks - 1) / chunks + pass - 1) / pass * pass);
+    const long long rows = M / chunks, whole = rows > pass ? 2ll * pass : pass;  // (a thread's two rows at once, where it has as many)
+    g.rows = (int)(rows < whole ? whole : rows / whole * whole);
     g.chunks = (int)(((long long)M + g.rows - 1) / g.rows);
     return g;
 }
@@ -375,7 +377,7 @@ static int backward(const linear_rows* dy, const linear_rows* x, const linear_ro
             const float* from = sums;
             int chunks = b.slope.chunks;
             void* list[] = {&from, &chunks, &N, &dbias};
-            if (const int rc = launch((const void*)bias_kernel, dim3((N + 31) / 32), 256, list, stream)) return rc;
+            if (const int rc = launch((const void*)bias_kernel, dim3((N + 31) / 32), 1024, list, stream)) return rc;
         }
     }
     const char* const g = b.dz ? dz : (const char*)dy->data;

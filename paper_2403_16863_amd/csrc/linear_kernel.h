@@ -343,13 +343,16 @@ __global__ __launch_bounds__(TL::WM * TL::WN * TL::WK * 64, (TL::OCC * TL::WM * 
     //   FREED     all of the stage's fragments are in registers, in all waves: its buffer takes the loads of stage t + NB from here on, load l at slot(l)
     //   LANDED    the loads of stage t + 1 are there, of all waves; its first step's fragments are read
     // With three buffers and more both are one barrier, ahead of the second step.  With two the loads have to go out and land within the stage between two such
-    // barriers, and half of that is the time that 64 KB take to come; a barrier of its own for each gives them the one and a half stages from FREED to LANDED.
-    constexpr int S = MT * NT, R = MT + NT, READS = NB == 2 ? S / 4 : S / 2 > R ? R : (S + 1) / 2;  // (products among which a step's fragments are read)
-    constexpr int FREED = NB == 2 ? S * 3 / 8 : S, LANDED = NB == 2 ? S + S * 5 / 8 : S;
-    constexpr int FIRST = NB == 2 ? FREED : S + S / 4, SPAN = NB == 2 ? S * 3 / 2 : 2 * S - S / 4;
+    // barriers, and half of that is the time that 64 KB take to come; a barrier of its own for each gives them longer, from FREED to the next stage's LANDED.
+    // (256 x 256 tiles, bfloat16, us, with one barrier / with two and the reads among a quarter of a step / five eighths, as here: 4096 x 16384 x 4096 with k along both
+    // 430 / 417 / 404, the other layouts 435 / 427 / 410 and 435 / 435 / 416; reads in a lump meet those of the unit's other waves.  The vendor's library takes
+    // 360, 412 and 485.  Four waves of 128 x 128 read a third less and take 414 to 425.)
+    constexpr int S = MT * NT, R = MT + NT, READS = NB == 2 ? S * 5 / 8 : S / 2 > R ? R : (S + 1) / 2;  // (products among which a step's fragments are read)
+    constexpr int FREED = NB == 2 ? S * 6 / 8 : S, LANDED = NB == 2 ? S + S * 3 / 8 : S;
+    constexpr int FIRST = NB == 2 ? FREED : S + S / 4, SPAN = NB == 2 ? S * 10 / 8 : 2 * S - S / 4;
     auto slot = [](int l) constexpr { return FIRST + l * SPAN / LPS; };
     auto before = [=](int at) constexpr { int n = 0; for (int l = 0; l < LPS; ++l) n += slot(l) < at; return n; };
-    static_assert(NB > 2 || (FREED > READS && FIRST + SPAN <= 2 * S && LANDED + READS < 2 * S), "a stage's own work ends with it");
+    static_assert(NB > 2 || (FREED >= READS && FIRST + SPAN <= 2 * S && LANDED + READS <= 2 * S), "a stage's own work ends with it");
 #pragma unroll
     for (int t = 0; t < NB; ++t) {
         next_stage(t);
