@@ -108,11 +108,11 @@ __global__ __launch_bounds__(1024) void bias_kernel(const float* sums, int chunk
 //     ceil(K / kstage) * max(ceil(n / occ) * alone, n * full) * (1 + load * f) * (1 + off_a) * (1 + off_b) * (1 + tokens) + n * ends + base + MB of C * out    (us)
 // (load: what the units take from each other; off_a, off_b: where rows of A, of B do not all begin on a line of 128 bytes; tokens: by rows of k, where A is read
 // by the transposing reads; ends: prologue and epilogue of a tile; out: the result's way to memory) and in ranges of k, whose MB of C are those of all parts in 32 bits,
-// a second launch and their reading in addition.  Fitted to the times of 9483 drawn products, M 1 .. 8192, N, K 8 .. 16384, in the three layouts, each on most tiles
-// and up to ten numbers of ranges, three sets of buffers in turn.  The standard deviation of time over model is 8 to 12 % by tile; what the model chooses
-// takes 2.4 % longer than the best that was measured (geometric mean; 14 % in the worst twentieth), with 64 x 64 tiles alone, which are the best for most, 12 %.
-// Each of the others is worth 0.05 to 0.6 % of that mean, and 10 to 15 % in its own range (779 x 1408 x 3904: 96 x 64 tiles on eight waves 17.6 us, the next best 21.0);
-// tiles of 64 x 128, 32 x 64 with k split four ways and 16 x 128 were built and gave nothing.
+// a second launch and their reading in addition.  Fitted to the times of 8951 drawn products, M 1 .. 8192, N, K 8 .. 16384 and up to 3e11 multiplications, in the three
+// layouts, each on the tiles that could be its best and up to ten numbers of ranges, three sets of buffers in turn.  The standard deviation of time over model is 9 to 13 % by
+// tile; what the model chooses takes 1.8 % longer than the best that was measured (geometric mean; 12 % in the worst twentieth).  Each tile but the 64 x 64 is worth 0.05 to 0.6 % of
+// that mean, and 10 to 15 % in its own range (779 x 1408 x 3904: 96 x 64 tiles on eight waves 17.6 us, the next best 21.0); without 64 x 64 it is 2.7 %, with it alone 9 %
+// longer.  Tiles of 64 x 128, 32 x 64 with k split four ways and 16 x 128 were built and gave nothing.
 struct Shape {
     int bm, bn, bk, wk, threads, occ;
     float alone, full, load, ends, off_a, off_b, tokens, base, out;
@@ -123,19 +123,19 @@ constexpr Shape shape(float alone, float full, float load, float ends, float off
     return {T::BM, T::BN, T::BK, T::WK, T::WM * T::WN * T::WK * 64, T::OCC, alone, full, load, ends, off_a, off_b, tokens, base, out};
 }
 static constexpr Shape kShapes[kTiles] = {
-    shape<0>(0.383f, 0.243f, 1.717f, 1.350f, 0.053f, 0.074f, 0.250f, 2.139f, 0.000f),
-    shape<1>(0.316f, 0.143f, 1.937f, 0.984f, 0.051f, 0.170f, 0.097f, 2.245f, 0.129f),
-    shape<2>(0.218f, 0.171f, 1.484f, 0.788f, 0.004f, 0.093f, 0.082f, 2.407f, 0.000f),
-    shape<3>(0.163f, 0.208f, 0.283f, 0.202f, 0.032f, 0.041f, -0.011f, 2.829f, 0.155f),
-    shape<4>(0.256f, 0.209f, 0.828f, 1.669f, 0.076f, 0.106f, 0.105f, 1.997f, 0.262f),
-    shape<5>(0.318f, 0.056f, 0.609f, 1.967f, 0.030f, 0.090f, 0.250f, 2.056f, 0.302f),
-    shape<6>(0.241f, 0.182f, 0.452f, 0.673f, 0.039f, 0.018f, 0.144f, 2.831f, 0.171f),
-    shape<7>(0.328f, 0.325f, 0.409f, 1.642f, 0.035f, -0.007f, 0.115f, 2.332f, 0.204f),
-    shape<8>(0.400f, 0.303f, 0.415f, 1.094f, 0.037f, -0.012f, 0.091f, 2.704f, 0.109f),
-    shape<9>(0.503f, 0.498f, 0.089f, 2.783f, 0.048f, -0.018f, 0.114f, 1.846f, 0.147f),
-    shape<10>(0.605f, 0.032f, 0.039f, 3.645f, 0.032f, -0.022f, 0.064f, 1.500f, 0.125f),
-    shape<11>(0.853f, 0.820f, 0.000f, 4.652f, 0.014f, -0.029f, 0.074f, 1.500f, 0.097f),
-    shape<12>(1.087f, 0.290f, 0.000f, 5.369f, 0.012f, -0.028f, 0.071f, 1.500f, 0.062f)};
+    shape<0>(0.373f, 0.325f, 1.676f, 1.370f, 0.022f, 0.093f, 0.317f, 2.121f, 0.000f),
+    shape<1>(0.312f, 0.210f, 1.680f, 0.824f, 0.035f, 0.192f, 0.132f, 2.412f, 0.493f),
+    shape<2>(0.214f, 0.224f, 0.866f, 0.393f, -0.012f, 0.114f, 0.115f, 2.837f, 0.187f),
+    shape<3>(0.161f, 0.196f, 0.194f, 0.103f, 0.049f, 0.096f, 0.011f, 2.956f, 0.207f),
+    shape<4>(0.249f, 0.099f, 0.787f, 1.574f, 0.090f, 0.123f, 0.111f, 2.103f, 0.292f),
+    shape<5>(0.310f, 0.280f, 0.709f, 1.881f, 0.055f, 0.099f, 0.207f, 2.141f, 0.297f),
+    shape<6>(0.229f, 0.209f, 0.559f, 0.130f, 0.127f, 0.080f, -0.009f, 3.352f, 0.203f),
+    shape<7>(0.318f, 0.317f, 0.661f, 1.158f, 0.093f, 0.029f, 0.005f, 2.795f, 0.206f),
+    shape<8>(0.385f, 0.308f, 0.575f, 0.767f, 0.082f, 0.036f, -0.008f, 2.905f, 0.115f),
+    shape<9>(0.496f, 0.441f, 0.367f, 2.776f, 0.114f, 0.019f, 0.004f, 1.927f, 0.108f),
+    shape<10>(0.588f, 0.463f, 0.462f, 3.727f, 0.083f, 0.016f, -0.025f, 1.500f, 0.085f),
+    shape<11>(0.755f, 0.449f, 0.503f, 4.709f, 0.067f, 0.002f, -0.027f, 1.500f, 0.052f),
+    shape<12>(0.983f, 0.478f, 0.448f, 5.549f, 0.060f, -0.005f, 0.005f, 1.500f, 0.000f)};
 
 constexpr long long kUnits = 256, kPartBytes = 64ll << 20;
 constexpr int kMostRanges = 32;
@@ -163,7 +163,7 @@ static float time_of(const Shape& s, long long tiles, int M, int N, const Plan& 
     const float alone = (float)((n + s.occ - 1) / s.occ) * s.alone, full = (float)n * s.full, filled = (float)tiles / ((float)n * kUnits);
     const float us = (float)stages * (alone > full ? alone : full) * (1.f + s.load * filled) * factor + (float)n * s.ends + s.base;
     const float mb = 1e-6f * (float)M * (float)N;
-    return parts ? us + 2.10f + 4.f * (float)p.ranges * mb * (0.55f + s.out) : us + 2.f * mb * s.out;
+    return parts ? us + 2.10f + 4.f * (float)p.ranges * mb * (0.45f + s.out) : us + 2.f * mb * s.out;
 }
 
 static Plan choose(int M, int N, int K, int layout, bool memory) {

