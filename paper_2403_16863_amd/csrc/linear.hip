@@ -108,11 +108,11 @@ __global__ __launch_bounds__(1024) void bias_kernel(const float* sums, int chunk
 //     ceil(K / kstage) * max(ceil(n / occ) * alone, n * full) * (1 + load * f) * (1 + off_a) * (1 + off_b) * (1 + tokens) + n * ends + base + MB of C * out    (us)
 // (load: what the units take from each other; off_a, off_b: where rows of A, of B do not all begin on a line of 128 bytes; tokens: by rows of k, where A is read
 // by the transposing reads; ends: prologue and epilogue of a tile; out: the result's way to memory) and in ranges of k, whose MB of C are those of all parts in 32 bits,
-// a second launch and their reading in addition.  Fitted to the times of 8951 drawn products, M 1 .. 8192, N, K 8 .. 16384 and up to 3e11 multiplications, in the three
+// a second launch and their reading in addition.  Fitted to the times of 10091 drawn products, M 1 .. 8192, N, K 8 .. 16384 and up to 3e11 multiplications, in the three
 // layouts, each on the tiles that could be its best and up to ten numbers of ranges, three sets of buffers in turn.  The standard deviation of time over model is 9 to 13 % by
-// tile; what the model chooses takes 1.8 % longer than the best that was measured (geometric mean; 12 % in the worst twentieth).  Each tile but the 64 x 64 is worth 0.05 to 0.6 % of
-// that mean, and 10 to 15 % in its own range (779 x 1408 x 3904: 96 x 64 tiles on eight waves 17.6 us, the next best 21.0); without 64 x 64 it is 2.7 %, with it alone 9 %
-// longer.  Tiles of 64 x 128, 32 x 64 with k split four ways and 16 x 128 were built and gave nothing.
+// tile; what the model chooses takes 1.9 % longer than the best that was measured (geometric mean; 12 % in the worst twentieth).  Each tile but the 64 x 64, without
+// which it is 4 %, is worth 0.05 to 1.4 % of that mean, and 10 to 15 % in its own range (779 x 1408 x 3904: 96 x 64 tiles on eight waves 17.6 us, the next best 21.0).
+// Tiles of 64 x 128, 32 x 64 with k split four ways and 16 x 128 were built and gave nothing, and neither did rings of one stage more, up to the whole LDS.
 struct Shape {
     int bm, bn, bk, wk, threads, occ;
     float alone, full, load, ends, off_a, off_b, tokens, base, out;
@@ -123,19 +123,20 @@ constexpr Shape shape(float alone, float full, float load, float ends, float off
     return {T::BM, T::BN, T::BK, T::WK, T::WM * T::WN * T::WK * 64, T::OCC, alone, full, load, ends, off_a, off_b, tokens, base, out};
 }
 static constexpr Shape kShapes[kTiles] = {
-    shape<0>(0.373f, 0.325f, 1.676f, 1.370f, 0.022f, 0.093f, 0.317f, 2.121f, 0.000f),
-    shape<1>(0.312f, 0.210f, 1.680f, 0.824f, 0.035f, 0.192f, 0.132f, 2.412f, 0.493f),
-    shape<2>(0.214f, 0.224f, 0.866f, 0.393f, -0.012f, 0.114f, 0.115f, 2.837f, 0.187f),
-    shape<3>(0.161f, 0.196f, 0.194f, 0.103f, 0.049f, 0.096f, 0.011f, 2.956f, 0.207f),
-    shape<4>(0.249f, 0.099f, 0.787f, 1.574f, 0.090f, 0.123f, 0.111f, 2.103f, 0.292f),
-    shape<5>(0.310f, 0.280f, 0.709f, 1.881f, 0.055f, 0.099f, 0.207f, 2.141f, 0.297f),
-    shape<6>(0.229f, 0.209f, 0.559f, 0.130f, 0.127f, 0.080f, -0.009f, 3.352f, 0.203f),
-    shape<7>(0.318f, 0.317f, 0.661f, 1.158f, 0.093f, 0.029f, 0.005f, 2.795f, 0.206f),
-    shape<8>(0.385f, 0.308f, 0.575f, 0.767f, 0.082f, 0.036f, -0.008f, 2.905f, 0.115f),
-    shape<9>(0.496f, 0.441f, 0.367f, 2.776f, 0.114f, 0.019f, 0.004f, 1.927f, 0.108f),
-    shape<10>(0.588f, 0.463f, 0.462f, 3.727f, 0.083f, 0.016f, -0.025f, 1.500f, 0.085f),
-    shape<11>(0.755f, 0.449f, 0.503f, 4.709f, 0.067f, 0.002f, -0.027f, 1.500f, 0.052f),
-    shape<12>(0.983f, 0.478f, 0.448f, 5.549f, 0.060f, -0.005f, 0.005f, 1.500f, 0.000f)};
+    shape<0>(0.381f, 0.226f, 1.755f, 1.334f, 0.034f, 0.092f, 0.202f, 2.156f, 0.193f),
+    shape<1>(0.309f, 0.119f, 1.936f, 0.724f, 0.006f, 0.227f, 0.078f, 2.504f, 0.633f),
+    shape<2>(0.218f, 0.221f, 1.177f, 0.339f, 0.010f, 0.080f, 0.004f, 2.876f, 0.217f),
+    shape<3>(0.170f, 0.201f, 0.293f, 0.078f, 0.039f, 0.053f, -0.018f, 2.955f, 0.199f),
+    shape<4>(0.247f, 0.162f, 0.859f, 1.537f, 0.082f, 0.112f, 0.099f, 2.157f, 0.296f),
+    shape<5>(0.308f, 0.269f, 0.754f, 1.798f, 0.054f, 0.088f, 0.213f, 2.186f, 0.317f),
+    shape<6>(0.228f, 0.207f, 0.584f, 0.000f, 0.103f, 0.077f, 0.014f, 3.371f, 0.236f),
+    shape<7>(0.314f, 0.291f, 0.680f, 0.939f, 0.080f, 0.029f, 0.022f, 2.937f, 0.231f),
+    shape<8>(0.380f, 0.295f, 0.658f, 0.691f, 0.073f, 0.038f, 0.002f, 2.893f, 0.124f),
+    shape<9>(0.492f, 0.489f, 0.370f, 2.748f, 0.118f, 0.019f, 0.009f, 1.941f, 0.111f),
+    shape<10>(0.584f, 0.030f, 0.464f, 3.730f, 0.086f, 0.012f, -0.022f, 1.500f, 0.087f),
+    shape<11>(0.752f, 0.670f, 0.504f, 4.693f, 0.070f, 0.001f, -0.027f, 1.500f, 0.053f),
+    shape<12>(0.981f, 0.964f, 0.452f, 5.508f, 0.060f, -0.004f, 0.007f, 1.500f, 0.000f),
+    shape<13>(0.261f, 0.220f, 1.615f, 0.473f, 0.037f, 0.067f, 0.169f, 2.564f, 0.122f)};
 
 constexpr long long kUnits = 256, kPartBytes = 64ll << 20;
 constexpr int kMostRanges = 32;
@@ -163,7 +164,7 @@ static float time_of(const Shape& s, long long tiles, int M, int N, const Plan& 
     const float alone = (float)((n + s.occ - 1) / s.occ) * s.alone, full = (float)n * s.full, filled = (float)tiles / ((float)n * kUnits);
     const float us = (float)stages * (alone > full ? alone : full) * (1.f + s.load * filled) * factor + (float)n * s.ends + s.base;
     const float mb = 1e-6f * (float)M * (float)N;
-    return parts ? us + 2.10f + 4.f * (float)p.ranges * mb * (0.45f + s.out) : us + 2.f * mb * s.out;
+    return parts ? us + 2.07f + 4.f * (float)p.ranges * mb * (0.45f + s.out) : us + 2.f * mb * s.out;
 }
 
 static Plan choose(int M, int N, int K, int layout, bool memory) {
