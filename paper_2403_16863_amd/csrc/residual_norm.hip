@@ -74,7 +74,7 @@ __device__ __forceinline__ void token_sums(float (&s)[K], float* meeting, int at
     for (int k = 0; k < K; ++k) s[k] = wave_sum(s[k]);
     if (W == 1) return;
     const int wave = threadIdx.x / 64 % W;
-    float* const mine = meeting + (at * 4 + group) * (W * 4);
+    float* const mine = meeting + (at * 8 + group) * (W * 4);
     if (threadIdx.x % 64 == 0) {
 #pragma unroll
         for (int k = 0; k < K; ++k) mine[wave * 4 + k] = s[k];
@@ -89,16 +89,17 @@ __device__ __forceinline__ void token_sums(float (&s)[K], float* meeting, int at
     }
 }
 
+// Tokens of a workgroup: eight waves' (forward on 2 x 4096 x 4096: 52.5 us with eight waves to a workgroup, 55.2 with four).
 template <int W>
 struct Block {
-    static constexpr int groups = W < 4 ? 4 / W : 1, threads = W * 64 * groups;
+    static constexpr int groups = W <= 4 ? 8 / W : 1, threads = W * 64 * groups;
 };
 
 // A lane's vectors of 8 channels: v * 64 W + lane of the token's lanes.
 template <bool BF, int W, int V>
 __global__ __launch_bounds__(Block<W>::threads) void forward_kernel(Args a) {
     constexpr int G = Block<W>::groups;
-    __shared__ float meeting[W > 1 ? 2 * 4 * W * 4 : 1];
+    __shared__ float meeting[W > 1 ? 2 * 8 * W * 4 : 1];
     const int group = threadIdx.x / (64 * W), lane = threadIdx.x % (64 * W);
     int c[V];
     bool in[V];
@@ -195,7 +196,7 @@ __global__ __launch_bounds__(Block<W>::threads) void forward_kernel(Args a) {
 template <bool BF, int W, int V>
 __global__ __launch_bounds__(Block<W>::threads) void backward_kernel(Args a) {
     constexpr int G = Block<W>::groups, LANES = 64 * W;
-    __shared__ float meeting[W > 1 ? 2 * 4 * W * 4 : 1];
+    __shared__ float meeting[W > 1 ? 2 * 8 * W * 4 : 1];
     __shared__ __attribute__((aligned(16))) float joined[G > 1 ? (G - 1) * LANES * V * 8 : 1];
     const int group = threadIdx.x / LANES, lane = threadIdx.x % LANES;
     int c[V];
@@ -441,22 +442,27 @@ __global__ __launch_bounds__(1024) void vector_sum_kernel(SumArgs a) {
 
 // ---- host side
 struct Kernel {
-    int most, waves;  // channels, waves of a token
+    int most, waves[2];  // channels; waves of a token, forward and backward
     const void *forward[2], *backward[2];
 };
-template <int W, int V>
+template <int W, int V, int WB = W, int VB = V>
 static constexpr Kernel kernel_of() {
-    return {512 * W * V, W, {(const void*)forward_kernel<false, W, V>, (const void*)forward_kernel<true, W, V>},
-            {(const void*)backward_kernel<false, W, V>, (const void*)backward_kernel<true, W, V>}};
+    static_assert(W * V == WB * VB, "as many channels both ways");
+    return {512 * W * V, {W, WB}, {(const void*)forward_kernel<false, W, V>, (const void*)forward_kernel<true, W, V>},
+            {(const void*)backward_kernel<false, WB, VB>, (const void*)backward_kernel<true, WB, VB>}};
 }
-static const Kernel kKernels[] = {kernel_of<1, 1>(), kernel_of<1, 2>(), kernel_of<1, 3>(), kernel_of<2, 2>(), kernel_of<4, 2>(), kernel_of<8, 2>(), kernel_of<8, 4>()};
+// One vector a lane up to 4096 channels: a backward pass is then 100 to 115 registers and four waves to a SIMD.  With more channels on fewer waves, and two waves to a
+// SIMD, it was 27.0 against 20.0 us on 3 x 1001 x 1152 (three vectors a lane), 50.3 against 41.7 on 2 x 4096 x 1536, 28.9 against 28.0 on 2 x 2048 x 2048 (two), and the
+// same on 2 x 4096 x 4096; on 2 x 2048 x 8192 sixteen waves with one vector each 110 against 98.5 on eight with two.  Beyond 8192 channels the backward pass spills (163 us for
+// 2048 x 12288 on eight waves, 210 on sixteen; forward 56 and 51).
+static const Kernel kKernels[] = {kernel_of<1, 1>(), kernel_of<2, 1>(), kernel_of<3, 1>(), kernel_of<4, 1>(), kernel_of<8, 1>(), kernel_of<8, 2>(), kernel_of<16, 2, 8, 4>()};
 
 static const Kernel& choose(int C) {
     int i = 0;
     while (kKernels[i].most < C) ++i;
     return kKernels[i];
 }
-static int groups_of(const Kernel& k) { return k.waves < 4 ? 4 / k.waves : 1; }
+static int groups_of(int waves) { return waves <= 4 ? 8 / waves : 1; }
 
 static bool given(const norm_tokens* t) { return t && t->data; }
 
@@ -523,18 +529,18 @@ static int launch(const void* fn, dim3 grid, int threads, void* args, void* stre
     return NORM_ELAUNCH;
 }
 
-// Units of a backward pass: two workgroups of four waves to a unit of the card are enough to keep its memory busy, and no more, for each has sums to
-// be added.
+// Units of a backward pass: as many workgroups as the card holds at once, and no more, for each has sums to be added (half as many, up to 4096 channels: 108.6 against
+// 97.8 us on 2 x 4096 x 4096; 768 in place of 512 21.8 against 18.0 on 3 x 1001 x 1152).
 struct Units {
     int runs, length, chunks, rows, blocks;
 };
 static Units units_of(int B, int N, int C, bool sequences) {
     const Kernel& k = choose(C);
-    const int groups = groups_of(k);
+    const int groups = groups_of(k.waves[1]);
     Units u;
     u.runs = sequences ? B : 1;
     u.length = sequences ? N : B * N;
-    const int limit = k.waves > 4 ? 256 : 512, each = u.runs >= limit ? 1 : limit / u.runs;
+    const int limit = k.most > 4096 ? 256 : 512, each = u.runs >= limit ? 1 : limit / u.runs;
     const long long most = ((long long)u.length + groups - 1) / groups, chunks = each < most ? each : most;
     u.rows = (int)((u.length + chunks - 1) / chunks + groups - 1) / groups * groups;
     u.chunks = (int)(((long long)u.length + u.rows - 1) / u.rows);
@@ -563,7 +569,7 @@ int residual_norm(const norm_tokens* x, const norm_tokens* h, const norm_tokens*
             return NORM_EINVAL;
     if (tokens_meet(y, z, false, B, N, C)) return NORM_EINVAL;
     const Kernel& k = choose(C);
-    const int groups = groups_of(k);
+    const int groups = groups_of(k.waves[0]);
     Args a = {};
     a.x = tokens(x, B, N), a.h = tokens(h, B, N), a.y = tokens(y, B, N), a.z = tokens(z, B, N);
     a.gate = v.gate, a.gate_stride = v.gate ? v.gate_stride : 0, a.gate_f32 = v.gate_f32, a.post = v.post_weight, a.pre = v.pre_weight, a.weight_f32 = v.weight_f32;
@@ -572,7 +578,7 @@ int residual_norm(const norm_tokens* x, const norm_tokens* h, const norm_tokens*
     const long long rounds = ((long long)a.length + groups - 1) / groups, blocks = rounds < 2048 ? rounds : 2048;
     a.rows = (int)((rounds + blocks - 1) / blocks) * groups;
     a.chunks = (int)(((long long)a.length + a.rows - 1) / a.rows);
-    return launch(k.forward[dtype], dim3(a.chunks), 64 * k.waves * groups, &a, stream);
+    return launch(k.forward[dtype], dim3(a.chunks), 64 * k.waves[0] * groups, &a, stream);
 }
 
 long long residual_norm_bwd_workspace(int B, int N, int C, int sequences) {
@@ -630,7 +636,7 @@ int residual_norm_bwd(const norm_tokens* dy, const norm_tokens* dz, const norm_t
     if (any) a.sums = (float*)workspace;
     float* const units = sequences && u.chunks > 1 ? (float*)workspace + 2ll * u.blocks * C : nullptr;
     if (sequences && dgate) a.units = units ? units : dgate;
-    if (const int rc = launch(k.backward[dtype], dim3(u.blocks), 64 * k.waves * groups_of(k), &a, stream)) return rc;
+    if (const int rc = launch(k.backward[dtype], dim3(u.blocks), 64 * k.waves[1] * groups_of(k.waves[1]), &a, stream)) return rc;
     if (!any) return NORM_OK;
     SumArgs s = {(float*)workspace, units, v.gate, v.post_weight, dgate, dpost_weight, dpre_weight, v.gate_f32, v.weight_f32, u.blocks, u.chunks, C, sequences};
     const int jobs = units && dgate ? 2 + B : 2;
