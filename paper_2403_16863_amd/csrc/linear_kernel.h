@@ -99,8 +99,14 @@ __device__ __forceinline__ void act8(float* v, int kind) {
     }
 }
 
+// Beyond 10^4 the smooth activations' slopes are 0 and 1 to all digits, and their terms, whose products would be infinity times 0, are formed there.  NaN stays.
+__device__ __forceinline__ float within(float v) { return v > 1e4f ? 1e4f : v < -1e4f ? -1e4f : v; }
+
 // g <- g act'(v)
-__device__ __forceinline__ void act_slope8(const float* v, float* g, int kind) {
+__device__ __forceinline__ void act_slope8(const float* values, float* g, int kind) {
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = kind == RELU ? values[i] : within(values[i]);
     if (kind == RELU) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) g[i] = v[i] > 0.f ? g[i] : v[i] <= 0.f ? 0.f : v[i];
