@@ -7,10 +7,8 @@
 //  * 16x16x32 MFMA, transposed product C^T += B^T A^T: a lane of the accumulator holds four consecutive n of one row of C.  Fragments of
 //    an operand with k along its rows are 16-byte reads of LDS, those of one by rows of k two transposing reads: the two operands are
 //    symmetric, so all layouts run one loop.
-//  * A ring of NB stages of BK values of k in LDS, filled by direct global -> LDS buffer loads, NB - 1 stages ahead of the products.  A
-//    stage is BK / 32 steps; each step multiplies the fragments that were read one step ago and reads the next step's, and the one barrier of a
-//    stage stands ahead of its last step, where all of its fragments are in registers.  Loads go out between the products: with
-//    two stages in the step behind the barrier, else spread from there to the next one.
+//  * A ring of NB stages of BK values of k in LDS, filled by direct global -> LDS buffer loads.  A stage is two steps; each multiplies the fragments that
+//    were read one step ago and reads the next step's, with the stage's loads and barriers between the products (where, is said at FREED and LANDED).
 //  * BK = 64: rows of 64 k are whole lines of 128 bytes.
 //  * Workgroups of WK groups of waves split the k of a tile among them, each with a ring of its own, and sum in LDS in group order; a group
 //    of one wave needs no barrier.  For few rows, where the weight's bytes are all that counts, such groups keep most of LDS in flight.
@@ -64,17 +62,18 @@ __device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf
 __device__ __forceinline__ float sigmoid_of_cubic(float z) {
     return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * fmaf(z * z, -0.10294324f, -2.3022082f)));
 }
-// The normal distribution's integral from -inf to z, and in *density its density.  With x = |z| / sqrt 2 and t = 1 / (1 + 0.38 x), e^(x^2) erfc(x) is a
-// polynomial in t (Hastings' form) to 2e-6 of itself, its coefficients fitted to the least relative error over 0 .. 20: the tail
+// The normal distribution's integral from -inf to z, and in *density its density.  With x = |z| / sqrt 2 and t = 1 / (1 + 0.44 x), e^(x^2) erfc(x) is a
+// polynomial in t (Hastings' form) to 5e-7 of itself, its coefficients fitted to the least relative error over 0 .. 20: the tail
 // keeps its digits for negative z, where 1 + erf loses them, at a third of the library function's instructions.
 __device__ __forceinline__ float normal(float z, float* density) {
-    const float e = __builtin_amdgcn_exp2f(z * z * -0.72134752044448170f), t = __builtin_amdgcn_rcpf(fmaf(0.26870057685088805f, fabsf(z), 1.f));
-    float y = fmaf(-0.1221754432f, t, 0.325358889f);
-    y = fmaf(y, t, -0.05603825632f);
-    y = fmaf(y, t, 0.2388010393f);
-    y = fmaf(y, t, 0.1836745718f);
-    y = fmaf(y, t, 0.2160605577f);
-    y = fmaf(y, t, 0.2143203926f);
+    const float e = __builtin_amdgcn_exp2f(z * z * -0.72134752044448170f), t = __builtin_amdgcn_rcpf(fmaf(0.31112698372208092f, fabsf(z), 1.f));
+    float y = fmaf(0.06935601595f, t, -0.2710227993f);
+    y = fmaf(y, t, 0.2862967791f);
+    y = fmaf(y, t, -0.01209306972f);
+    y = fmaf(y, t, 0.2123377131f);
+    y = fmaf(y, t, 0.2181195787f);
+    y = fmaf(y, t, 0.2487810698f);
+    y = fmaf(y, t, 0.2482244134f);
     const float tail = 0.5f * e * (y * t);
     *density = 0.3989422804014327f * e;
     return z < 0.f ? tail : 1.f - tail;
