@@ -16,8 +16,8 @@ __global__ __launch_bounds__(64) void join_kernel(const float* parts, Args p, in
     if (i >= chunks) return;
     const unsigned row = (unsigned)p.N / 8, m = i / row, n = (i - m * row) * 8;
     float bias[8];
-    load_bias<T>(p.e, (int)n, true, bias);
-    const u32x4 residual = load_residual(p.e, (int)m, (int)n, true);
+    load_bias<T, 8>(p.e, (int)n, true, bias);
+    const u32x4 residual = load_residual<8>(p.e, (int)m, (int)n, true);
     const f32x4* src = reinterpret_cast<const f32x4*>(parts) + (size_t)i * 2;
     f32x4 x = src[0], y = src[1];
 #pragma unroll 4
@@ -27,7 +27,7 @@ __global__ __launch_bounds__(64) void join_kernel(const float* parts, Args p, in
         y += src[1];
     }
     float v[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
-    finish8<T>(p.e, (uint16_t*)p.out, p.ldo, (int)m, (int)n, v, bias, residual);
+    finish<T, 8>(p.e, (uint16_t*)p.out, p.ldo, (int)m, (int)n, v, bias, residual);
 }
 
 // dz = dy act'(pre), rounded, and the rows' sums for dbias, in one pass over dy and pre: memory binds.  A workgroup has 256 / lanes rows of `lanes` vectors of 8
@@ -63,11 +63,11 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a) {
             for (int r = 0; r < AT_ONCE; ++r) {
                 const long long m = m0 + r * step;
                 float g[8], v[8];
-                unpack8<T>(gr[r], g);
+                unpack<T, 8>(gr[r], g);
                 if (a.act) {
-                    unpack8<T>(vr[r], v);
+                    unpack<T, 8>(vr[r], v);
                     act_slope8(v, g, a.act);
-                    if (a.dz && m < end) *(u32x4*)(a.dz + m * a.N + n) = pack8<T>(g);
+                    if (a.dz && m < end) *(u32x4*)(a.dz + m * a.N + n) = pack<T, 8>(g);
                 }
 #pragma unroll
                 for (int i = 0; i < 8; ++i) sum[i] += g[i];
@@ -105,38 +105,40 @@ __global__ __launch_bounds__(1024) void bias_kernel(const float* sums, int chunk
 }
 
 // ---- choice of the tile.  With n tiles on the busiest of the 256 units, and f of the units' n rounds filled, a product takes about
-//     ceil(K / kstage) * max(ceil(n / occ) * alone, n * full) * (1 + load * f) * (1 + off_a) * (1 + off_b) * (1 + tokens) + n * ends + base + MB of C * out    (us)
-// (load: what the units take from each other; off_a, off_b: where rows of A, of B do not all begin on a line of 128 bytes; tokens: by rows of k, where A is read
-// by the transposing reads; ends: prologue and epilogue of a tile; out: the result's way to memory) and in ranges of k, whose MB of C are those of all parts in 32 bits,
-// a second launch and their reading in addition.  Fitted to the times of 10091 drawn products, M 1 .. 8192, N, K 8 .. 16384 and up to 3e11 multiplications, in the three
+//     ceil(K / kstage) * max(ceil(n / occ) * alone, n * full) * (1 + load * f) * (1 + off_a) * (1 + off_b) * (1 + tokens) * (1 + by_k) + n * ends + base + MB of C * out    (us)
+// (load: what the units take from each other; off_a, off_b: where rows of A, of B do not all begin on a line of 128 bytes; tokens, by_k: where A, B lie by rows of k, and are read
+// by the transposing reads, and in short pieces of a row by narrow tiles; ends: prologue and epilogue of a tile; out: the result's way to memory) and in ranges of k, whose MB of C are those of all parts in 32 bits,
+// a second launch and their reading in addition.  Fitted to the times of 12437 drawn products, M 1 .. 8192, N, K 8 .. 16384 and up to 3e11 multiplications, in the three
 // layouts, each on the tiles that could be its best and up to ten numbers of ranges, three sets of buffers in turn.  The standard deviation of time over model is 9 to 13 % by
-// tile; what the model chooses takes 1.9 % longer than the best that was measured (geometric mean; 12 % in the worst twentieth).  Each tile but the 64 x 64, without
-// which it is 4 %, is worth 0.05 to 1.4 % of that mean, and 10 to 15 % in its own range (779 x 1408 x 3904: 96 x 64 tiles on eight waves 17.6 us, the next best 21.0).
+// tile; what the model chooses takes 2.0 % longer than the best that was measured (geometric mean; 12 % in the worst twentieth).  Each tile but the 64 x 64, without
+// which it is 4 %, is worth up to 1.4 % of that mean, and 10 to 15 % in its own range (779 x 1408 x 3904: 96 x 64 tiles on eight waves 17.6 us, the next best 21.0; 4 rows, 8192 -> 2048, k
+// along both: 16 x 16 tiles 8.5, the next best 10.4).
 // Tiles of 64 x 128, 32 x 64 with k split four ways and 16 x 128 were built and gave nothing, and neither did rings of one stage more, up to the whole LDS.
 struct Shape {
     int bm, bn, bk, wk, threads, occ;
-    float alone, full, load, ends, off_a, off_b, tokens, base, out;
+    float alone, full, load, ends, off_a, off_b, tokens, base, out, by_k;
 };
 template <int I>
-constexpr Shape shape(float alone, float full, float load, float ends, float off_a, float off_b, float tokens, float base, float out) {
+constexpr Shape shape(float alone, float full, float load, float ends, float off_a, float off_b, float tokens, float base, float out, float by_k) {
     using T = TileOf<I>;
-    return {T::BM, T::BN, T::BK, T::WK, T::WM * T::WN * T::WK * 64, T::OCC, alone, full, load, ends, off_a, off_b, tokens, base, out};
+    return {T::BM, T::BN, T::BK, T::WK, T::WM * T::WN * T::WK * 64, T::OCC, alone, full, load, ends, off_a, off_b, tokens, base, out, by_k};
 }
 static constexpr Shape kShapes[kTiles] = {
-    shape<0>(0.381f, 0.226f, 1.755f, 1.334f, 0.034f, 0.092f, 0.202f, 2.156f, 0.193f),
-    shape<1>(0.309f, 0.119f, 1.936f, 0.724f, 0.006f, 0.227f, 0.078f, 2.504f, 0.633f),
-    shape<2>(0.218f, 0.221f, 1.177f, 0.339f, 0.010f, 0.080f, 0.004f, 2.876f, 0.217f),
-    shape<3>(0.170f, 0.201f, 0.293f, 0.078f, 0.039f, 0.053f, -0.018f, 2.955f, 0.199f),
-    shape<4>(0.247f, 0.162f, 0.859f, 1.537f, 0.082f, 0.112f, 0.099f, 2.157f, 0.296f),
-    shape<5>(0.308f, 0.269f, 0.754f, 1.798f, 0.054f, 0.088f, 0.213f, 2.186f, 0.317f),
-    shape<6>(0.228f, 0.207f, 0.584f, 0.000f, 0.103f, 0.077f, 0.014f, 3.371f, 0.236f),
-    shape<7>(0.314f, 0.291f, 0.680f, 0.939f, 0.080f, 0.029f, 0.022f, 2.937f, 0.231f),
-    shape<8>(0.380f, 0.295f, 0.658f, 0.691f, 0.073f, 0.038f, 0.002f, 2.893f, 0.124f),
-    shape<9>(0.492f, 0.489f, 0.370f, 2.748f, 0.118f, 0.019f, 0.009f, 1.941f, 0.111f),
-    shape<10>(0.584f, 0.030f, 0.464f, 3.730f, 0.086f, 0.012f, -0.022f, 1.500f, 0.087f),
-    shape<11>(0.752f, 0.670f, 0.504f, 4.693f, 0.070f, 0.001f, -0.027f, 1.500f, 0.053f),
-    shape<12>(0.981f, 0.964f, 0.452f, 5.508f, 0.060f, -0.004f, 0.007f, 1.500f, 0.000f),
-    shape<13>(0.261f, 0.220f, 1.615f, 0.473f, 0.037f, 0.067f, 0.169f, 2.564f, 0.122f)};
+    shape<0>(0.338f, 0.109f, 1.643f, 1.297f, 0.012f, 0.117f, 0.062f, 2.175f, 0.220f, 0.371f),
+    shape<1>(0.294f, 0.168f, 1.984f, 0.775f, 0.008f, 0.226f, 0.050f, 2.447f, 0.411f, 0.103f),
+    shape<2>(0.203f, 0.204f, 1.249f, 0.357f, 0.025f, 0.092f, -0.054f, 2.817f, 0.181f, 0.125f),
+    shape<3>(0.171f, 0.195f, 0.342f, 0.036f, 0.052f, 0.048f, -0.043f, 2.946f, 0.207f, 0.042f),
+    shape<4>(0.231f, 0.110f, 0.916f, 1.495f, 0.069f, 0.106f, 0.034f, 2.179f, 0.315f, 0.131f),
+    shape<5>(0.296f, 0.144f, 0.779f, 1.804f, 0.047f, 0.081f, 0.169f, 2.175f, 0.321f, 0.085f),
+    shape<6>(0.227f, 0.202f, 0.589f, 0.000f, 0.085f, 0.065f, 0.024f, 3.299f, 0.250f, 0.031f),
+    shape<7>(0.325f, 0.176f, 0.660f, 0.803f, 0.065f, 0.024f, 0.065f, 3.026f, 0.251f, -0.048f),
+    shape<8>(0.382f, 0.293f, 0.680f, 0.545f, 0.074f, 0.032f, 0.017f, 2.967f, 0.143f, -0.010f),
+    shape<9>(0.496f, 0.496f, 0.367f, 2.551f, 0.112f, 0.017f, 0.031f, 2.094f, 0.127f, -0.022f),
+    shape<10>(0.602f, 0.573f, 0.455f, 3.706f, 0.077f, 0.011f, 0.009f, 1.500f, 0.092f, -0.047f),
+    shape<11>(0.769f, 0.003f, 0.495f, 4.676f, 0.063f, -0.001f, -0.006f, 1.500f, 0.058f, -0.032f),
+    shape<12>(0.980f, 0.145f, 0.449f, 5.520f, 0.055f, -0.007f, 0.005f, 1.500f, 0.002f, 0.009f),
+    shape<13>(0.229f, 0.190f, 1.636f, 0.504f, 0.039f, 0.080f, 0.068f, 2.534f, 0.082f, 0.246f),
+    shape<14>(0.226f, 0.028f, 1.295f, 1.450f, -0.011f, 0.076f, 0.156f, 1.847f, 0.189f, 0.800f)};
 
 constexpr long long kUnits = 256, kPartBytes = 64ll << 20;
 constexpr int kMostRanges = 32;
@@ -164,7 +166,7 @@ static float time_of(const Shape& s, long long tiles, int M, int N, const Plan& 
     const float alone = (float)((n + s.occ - 1) / s.occ) * s.alone, full = (float)n * s.full, filled = (float)tiles / ((float)n * kUnits);
     const float us = (float)stages * (alone > full ? alone : full) * (1.f + s.load * filled) * factor + (float)n * s.ends + s.base;
     const float mb = 1e-6f * (float)M * (float)N;
-    return parts ? us + 2.07f + 4.f * (float)p.ranges * mb * (0.45f + s.out) : us + 2.f * mb * s.out;
+    return parts ? us + 2.13f + 4.f * (float)p.ranges * mb * (0.44f + s.out) : us + 2.f * mb * s.out;
 }
 
 static Plan choose(int M, int N, int K, int layout, bool memory) {
@@ -175,7 +177,7 @@ static Plan choose(int M, int N, int K, int layout, bool memory) {
         const Shape& s = kShapes[t];
         if (!fits(s, M, N, 1)) continue;
         const long long tiles = tiles_of(s, M, N);
-        const float factor = (off_a ? 1.f + s.off_a : 1.f) * (off_b ? 1.f + s.off_b : 1.f) * (layout == TOKENS ? 1.f + s.tokens : 1.f);
+        const float factor = (off_a ? 1.f + s.off_a : 1.f) * (off_b ? 1.f + s.off_b : 1.f) * (layout == TOKENS ? 1.f + s.tokens : 1.f) * (layout != ROWS_N ? 1.f + s.by_k : 1.f);
         for (int r : {1, 2, 3, 4, 6, 8, 12, 16, 24, kMostRanges}) {
             if (r > 1 && (!memory || tiles * r > kUnits * s.occ || (long long)r * 128 > K)) break;
             const Plan p = r > 1 ? plan_of(t, M, N, K, r) : Plan{t, 1, K, 0};

@@ -44,17 +44,7 @@ struct BF16 {
     static __device__ __forceinline__ void unpack2(unsigned w, float* x) { x[0] = __uint_as_float(w << 16), x[1] = __uint_as_float(w & 0xffff0000u); }
 };
 
-template <class T>
-__device__ __forceinline__ void unpack8(u32x4 w, float* x) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) T::unpack2(w[i], x + 2 * i);
-}
-template <class T>
-__device__ __forceinline__ u32x4 pack8(const float* x) {
-    return u32x4{T::pack2(x[0], x[1]), T::pack2(x[2], x[3]), T::pack2(x[4], x[5]), T::pack2(x[6], x[7])};
-}
-
-// The activations of eight values.  In 32 bits with the hardware's exponential (2^x) and reciprocal, each good to a step or so: the results
+// The activations of a lane's values.  In 32 bits with the hardware's exponential (2^x) and reciprocal, each good to a step or so: the results
 // are rounded to 16 bits.  z = -inf gives NaN in silu and both gelu, -inf times 0, as their formulas do.
 __device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.4426950408889634f)); }
 // sigmoid(2 v) of the tanh form's argument v = sqrt(2 / pi) (z + 0.044715 z^3): tanh v = 2 sigmoid(2 v) - 1, so the form is z times it: one
@@ -79,22 +69,23 @@ __device__ __forceinline__ float normal(float z, float* density) {
     return z < 0.f ? tail : 1.f - tail;
 }
 
-__device__ __forceinline__ void act8(float* v, int kind) {
+template <int W>
+__device__ __forceinline__ void activate(float* v, int kind) {
     if (kind == RELU) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = v[i] < 0.f ? 0.f : v[i];
+        for (int i = 0; i < W; ++i) v[i] = v[i] < 0.f ? 0.f : v[i];
     } else if (kind == SILU) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] *= sigmoid(v[i]);
+        for (int i = 0; i < W; ++i) v[i] *= sigmoid(v[i]);
     } else if (kind == GELU) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < W; ++i) {
             float density;
             v[i] *= normal(v[i], &density);
         }
     } else if (kind == GELU_TANH) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] *= sigmoid_of_cubic(v[i]);
+        for (int i = 0; i < W; ++i) v[i] *= sigmoid_of_cubic(v[i]);
     }
 }
 
@@ -159,41 +150,56 @@ struct Args {
     Epilogue e;
 };
 
-// What the epilogue reads for eight consecutive columns of a row.  All of it is asked for ahead of the first store, behind which the compiler, which does
-// not know that they do not meet, would keep it: a load's time for each store.
-template <class T>
+// What the epilogue reads for W = 8 or 4 consecutive columns of a row.  All of it is asked for ahead of the first store, behind which the compiler, which
+// does not know that they do not meet, would keep it: a load's time for each store.
+template <int W>
+using Packed = std::conditional_t<W == 8, u32x4, u32x2>;
+template <class T, int W>
+__device__ __forceinline__ void unpack(Packed<W> w, float* x) {
+#pragma unroll
+    for (int i = 0; i < W / 2; ++i) T::unpack2(w[i], x + 2 * i);
+}
+template <class T, int W>
+__device__ __forceinline__ Packed<W> pack(const float* x) {
+    Packed<W> w;
+#pragma unroll
+    for (int i = 0; i < W / 2; ++i) w[i] = T::pack2(x[2 * i], x[2 * i + 1]);
+    return w;
+}
+template <class T, int W>
 __device__ __forceinline__ void load_bias(const Epilogue& e, int n, bool in, float* b) {
     if (in && e.bias && e.bias_f32) {
-        const float4 lo = ((const float4*)((const float*)e.bias + n))[0], hi = ((const float4*)((const float*)e.bias + n))[1];
-        b[0] = lo.x, b[1] = lo.y, b[2] = lo.z, b[3] = lo.w, b[4] = hi.x, b[5] = hi.y, b[6] = hi.z, b[7] = hi.w;
+#pragma unroll
+        for (int i = 0; i < W; i += 4) *(f32x4*)(b + i) = *(const f32x4*)((const float*)e.bias + n + i);
     } else if (in && e.bias) {
-        unpack8<T>(*(const u32x4*)((const uint16_t*)e.bias + n), b);
+        unpack<T, W>(*(const Packed<W>*)((const uint16_t*)e.bias + n), b);
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) b[i] = 0;
+        for (int i = 0; i < W; ++i) b[i] = 0;
     }
 }
-__device__ __forceinline__ u32x4 load_residual(const Epilogue& e, int m, int n, bool in) {
-    return in && e.residual ? *(const u32x4*)(e.residual + (size_t)m * e.ldr + n) : u32x4{0, 0, 0, 0};
+template <int W>
+__device__ __forceinline__ Packed<W> load_residual(const Epilogue& e, int m, int n, bool in) {
+    return in && e.residual ? *(const Packed<W>*)(e.residual + (size_t)m * e.ldr + n) : Packed<W>(0);
 }
 
-// Eight consecutive values of one row of C: bias, activation, residual, one rounding.
-template <class T>
-__device__ __forceinline__ void finish8(const Epilogue& e, uint16_t* out, int ldo, int m, int n, float* v, const float* bias, u32x4 residual) {
+// Consecutive values of one row of C: bias, activation, residual, one rounding.
+template <class T, int W>
+__device__ __forceinline__ void finish(const Epilogue& e, uint16_t* out, int ldo, int m, int n, float* v, const float* bias, Packed<W> residual) {
     if (e.bias) {  // (a sum without one keeps the sign of a zero)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] += bias[i];
+        for (int i = 0; i < W; ++i) v[i] += bias[i];
     }
     if (e.pre)  // (past the caches, for the backward pass: 4096 x 16384 x 4096 437 -> 428 us)
-        __builtin_nontemporal_store(pack8<T>(v), (u32x4*)(e.pre + (size_t)m * e.ldp + n));
-    act8(v, e.act);
+        __builtin_nontemporal_store(pack<T, W>(v), (Packed<W>*)(e.pre + (size_t)m * e.ldp + n));
+    activate<W>(v, e.act);
     if (e.residual) {
-        float r[8];
-        unpack8<T>(residual, r);
+        float r[W];
+        unpack<T, W>(residual, r);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] += r[i];
+        for (int i = 0; i < W; ++i) v[i] += r[i];
     }
-    *(u32x4*)(out + (size_t)m * ldo + n) = pack8<T>(v);
+    *(Packed<W>*)(out + (size_t)m * ldo + n) = pack<T, W>(v);
 }
 
 // One operand's piece of a stage: R rows (m or n) of BK values of k, or BK rows of R values.
@@ -270,7 +276,8 @@ __global__ __launch_bounds__(TL::WM * TL::WN * TL::WK * 64, (TL::OCC * TL::WM * 
     constexpr int LA = PA::LOADS, LB = PB::LOADS, LPS = LA + LB;
     constexpr int RING = NB * (PA::BYTES + PB::BYTES);
     static_assert(KS == 2, "fragments of a stage's two steps take turns");
-    static_assert(NT % 2 == 0, "C is stored in pairs of 16-column tiles");
+    constexpr int TOGETHER = NT % 2 ? 1 : 2, WIDE = 4 * TOGETHER;  // 16-column tiles whose values a lane stores at once, and how many those are
+    static_assert(NT == 1 || TOGETHER == 2, "C is stored in pairs of 16-column tiles, or it is one");
     static_assert(NB >= 2 && (NB - 1) * LPS <= 63, "the counted waits must fit s_waitcnt's field");
     static_assert(WK == 1 || RING >= BM * BN * 4, "a ring also holds its group's partial sums");
     static_assert(WK * RING <= 160 * 1024, "LDS of a compute unit");
@@ -358,7 +365,8 @@ __global__ __launch_bounds__(TL::WM * TL::WN * TL::WK * 64, (TL::OCC * TL::WM * 
     constexpr int FIRST = NB == 2 ? FREED : S + S / 4, SPAN = NB == 2 ? S * 10 / 8 : 2 * S - S / 4;
     auto slot = [](int l) constexpr { return FIRST + l * SPAN / LPS; };
     auto before = [=](int at) constexpr { int n = 0; for (int l = 0; l < LPS; ++l) n += slot(l) < at; return n; };
-    static_assert(NB > 2 || (FREED >= READS && FIRST + SPAN <= 2 * S && LANDED + READS <= 2 * S), "a stage's own work ends with it");
+    static_assert(FREED > (R - 1) * READS / R && LANDED + READS <= 2 * S, "a step's fragments are read before their buffer is freed, and within a stage");
+    static_assert(NB > 2 || FIRST + SPAN <= 2 * S, "with two buffers a stage's loads go out within one");
 #pragma unroll
     for (int t = 0; t < NB; ++t) {
         next_stage(t);
@@ -420,68 +428,75 @@ __global__ __launch_bounds__(TL::WM * TL::WN * TL::WK * 64, (TL::OCC * TL::WM * 
     // neighbouring tiles it has eight consecutive n.
     const int g = lane >> 4;
     auto row_of = [&](int mt) __attribute__((always_inline)) { return m0 + wm * TM + mt * 16 + (lane & 15); };
-    auto column_of = [&](int nt) __attribute__((always_inline)) { return n0 + wn * TN + nt * 16 + (PARTS ? g * 4 : (g & 1) * 16 + (g >> 1) * 8); };
-    auto store_pair = [&](int mt, int nt, f32x4 x, f32x4 y, const float* bias, u32x4 residual) __attribute__((always_inline)) {
+    auto column_of = [&](int nt) __attribute__((always_inline)) {
+        return n0 + wn * TN + nt * 16 + (PARTS || TOGETHER == 1 ? g * 4 : (g & 1) * 16 + (g >> 1) * 8);
+    };
+    auto store = [&](int mt, int nt, f32x4 x, f32x4 y, const float* bias, Packed<WIDE> residual) __attribute__((always_inline)) {
         const int m = row_of(mt), n = column_of(nt);
         if constexpr (PARTS) {
             float* const row = (float*)p.out + ((size_t)range * M + m) * N;
             if (m < M && n < N) *(f32x4*)(row + n) = x;
-            if (m < M && n + 16 < N) *(f32x4*)(row + n + 16) = y;
+            if (TOGETHER == 2 && m < M && n + 16 < N) *(f32x4*)(row + n + 16) = y;
             return;
         }
-        float v[8];
+        float v[WIDE];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(x[i]), __float_as_uint(y[i]), false, false);
-            v[i] = __uint_as_float(s[0]), v[4 + i] = __uint_as_float(s[1]);
+            if constexpr (TOGETHER == 2) {
+                const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(x[i]), __float_as_uint(y[i]), false, false);
+                v[i] = __uint_as_float(s[0]), v[4 + i] = __uint_as_float(s[1]);
+            } else {
+                v[i] = x[i];
+            }
         }
-        if (m < M && n < N) finish8<T>(p.e, (uint16_t*)p.out, p.ldo, m, n, v, bias, residual);
+        if (m < M && n < N) finish<T, WIDE>(p.e, (uint16_t*)p.out, p.ldo, m, n, v, bias, residual);
     };
+    constexpr int ACROSS = NT / TOGETHER, STORES = MT * ACROSS;
     if constexpr (WK == 1) {
-        float bias[NT / 2][8];
-        u32x4 residual[MT][NT / 2];
+        float bias[ACROSS][WIDE];
+        Packed<WIDE> residual[MT][ACROSS];
         if constexpr (!PARTS) {
 #pragma unroll
-            for (int q = 0; q < NT / 2; ++q) {
-                const int n = column_of(2 * q);
-                load_bias<T>(p.e, n, n < N, bias[q]);
+            for (int q = 0; q < ACROSS; ++q) {
+                const int n = column_of(TOGETHER * q);
+                load_bias<T, WIDE>(p.e, n, n < N, bias[q]);
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt) residual[mt][q] = load_residual(p.e, row_of(mt), n, n < N && row_of(mt) < M);
+                for (int mt = 0; mt < MT; ++mt) residual[mt][q] = load_residual<WIDE>(p.e, row_of(mt), n, n < N && row_of(mt) < M);
             }
         }
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-            for (int nt = 0; nt < NT; nt += 2) store_pair(mt, nt, acc[mt][nt], acc[mt][nt + 1], bias[nt / 2], residual[mt][nt / 2]);
+            for (int nt = 0; nt < NT; nt += TOGETHER) store(mt, nt, acc[mt][nt], acc[mt][nt + TOGETHER - 1], bias[nt / TOGETHER], residual[mt][nt / TOGETHER]);
     } else {
-        constexpr int PAIRS = MT * NT / 2, MINE = (PAIRS + WK - 1) / WK;
+        constexpr int MINE = (STORES + WK - 1) / WK;
         if constexpr (NW > 1) __syncthreads();  // the ring is shared by the group's waves
         f32x4* const mine = reinterpret_cast<f32x4*>(smem_b + wk * RING + wave * (TM * TN * 4)) + lane;
 #pragma unroll
         for (int i = 0; i < MT * NT; ++i) mine[i * 64] = acc[i / NT][i % NT];
-        float bias[MINE][8];
-        u32x4 residual[MINE];
+        float bias[MINE][WIDE];
+        Packed<WIDE> residual[MINE];
         if constexpr (!PARTS) {
 #pragma unroll
             for (int q = 0; q < MINE; ++q) {
-                const int pr = q * WK + wk, m = row_of(pr / (NT / 2)), n = column_of(pr % (NT / 2) * 2);
-                load_bias<T>(p.e, n, pr < PAIRS && n < N, bias[q]);
-                residual[q] = load_residual(p.e, m, n, pr < PAIRS && n < N && m < M);
+                const int at = q * WK + wk, m = row_of(at / ACROSS), n = column_of(at % ACROSS * TOGETHER);
+                load_bias<T, WIDE>(p.e, n, at < STORES && n < N, bias[q]);
+                residual[q] = load_residual<WIDE>(p.e, m, n, at < STORES && n < N && m < M);
             }
         }
         __syncthreads();
 #pragma unroll
         for (int q = 0; q < MINE; ++q) {
-            const int pr = q * WK + wk;
-            if (PAIRS % WK != 0 && pr >= PAIRS) break;
+            const int at = q * WK + wk;
+            if (STORES % WK != 0 && at >= STORES) break;
             f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int w = 0; w < WK; ++w) {
                 const f32x4* part = reinterpret_cast<const f32x4*>(smem_b + w * RING + wave * (TM * TN * 4)) + lane;
-                x += part[2 * pr * 64];
-                y += part[(2 * pr + 1) * 64];
+                x += part[TOGETHER * at * 64];
+                if (TOGETHER == 2) y += part[(2 * at + 1) * 64];
             }
-            store_pair(pr / (NT / 2), pr % (NT / 2) * 2, x, y, bias[q], residual[q]);
+            store(at / ACROSS, at % ACROSS * TOGETHER, x, y, bias[q], residual[q]);
         }
     }
 }

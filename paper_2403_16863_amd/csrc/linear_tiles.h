@@ -23,7 +23,8 @@ template <> struct TileOf<10> : Tile<128, 256, 64, 2, 4, 1, 3, 1> {};
 template <> struct TileOf<11> : Tile<192, 256, 64, 2, 4, 1, 2, 1> {};
 template <> struct TileOf<12> : Tile<256, 256, 64, 2, 4, 1, 2, 1> {};
 template <> struct TileOf<13> : Tile<32, 32, 64, 1, 1, 4, 2, 2> {};
-constexpr int kTiles = 14;
+template <> struct TileOf<14> : Tile<16, 16, 64, 1, 1, 8, 4, 1> {};
+constexpr int kTiles = 15;
 
 // Kernel of a tile; parts: a range of k into the workspace.
 template <int LAYOUT, bool BF>
