@@ -35,7 +35,7 @@ __global__ __launch_bounds__(64) void join_kernel(const float* parts, Args p, in
 struct SlopeArgs {
     const uint16_t *dy, *pre;
     uint16_t* dz;
-    float* sums;  // [chunk][N], or null
+    float* sums;  // [chunk][N] (one chunk: dbias itself), or null
     long long lddy, ldpre;
     int M, N, rows, lanes, act;
 };
@@ -251,7 +251,8 @@ struct Memory {
 
 static long long up(long long bytes) { return (bytes + 255) / 256 * 256; }
 
-// Workgroups of the activation's backward step: 1024 where there are rows enough for them to have two passes each.
+// Workgroups of the activation's backward step: 1024 where there are rows enough for them to have two passes each.  Up to four passes of rows are one chunk,
+// whose sums are dbias: that spares a launch.
 struct SlopeGrid {
     int lanes, blocks, rows, chunks;
 };
@@ -265,6 +266,7 @@ static SlopeGrid slope_grid(int M, int N) {
     const long long chunks = want < most ? want : most;
     const long long rows = M / chunks, whole = rows > pass ? 2ll * pass : pass;  // (a thread's two rows at once, where it has as many)
     g.rows = (int)(rows < whole ? whole : rows / whole * whole);
+    if (M <= 4 * pass) g.rows = 4 * pass;
     g.chunks = (int)(((long long)M + g.rows - 1) / g.rows);
     return g;
 }
@@ -285,7 +287,7 @@ static Backward backward_of(int M, int N, int K, int w_rows_of_n, int dw_rows_of
     if (dx) b.dx = choose(M, K, N, b.dx_layout, true);
     if (dw) b.dw = dw_rows_of_n ? choose(N, K, M, TOKENS, true) : choose(K, N, M, TOKENS, true);
     b.dz = activation && (dx || dw) ? up(2ll * M * N) : 0;
-    b.sums = dbias ? up(4ll * b.slope.chunks * N) : 0;
+    b.sums = dbias && b.slope.chunks > 1 ? up(4ll * b.slope.chunks * N) : 0;
     b.parts = b.dx.bytes > b.dw.bytes ? b.dx.bytes : b.dw.bytes;
     return b;
 }
@@ -325,7 +327,10 @@ static int forward(const linear_rows* x, const linear_rows* w, int w_rows_of_n, 
     a.lda = stride_of(x, M, K), a.ldb = stride_of(w, wr, wc), a.ldo = stride_of(out, M, N);
     a.e.bias = bias, a.e.bias_f32 = bias_f32, a.e.act = activation;
     if (given(residual)) a.e.residual = (const uint16_t*)residual->data, a.e.ldr = stride_of(residual, M, N);
-    if (given(pre)) a.e.pre = (uint16_t*)pre->data, a.e.ldp = stride_of(pre, M, N);
+    if (given(pre)) {
+        a.e.pre = (uint16_t*)pre->data, a.e.ldp = stride_of(pre, M, N);
+        a.e.pre_lines = (uintptr_t)pre->data % 128 == 0 && a.e.ldp % 64 == 0;
+    }
     return run(plan, layout, dtype, a, workspace, stream);
 }
 
@@ -372,11 +377,11 @@ static int backward(const linear_rows* dy, const linear_rows* x, const linear_ro
         s.pre = s.dy;
         if (activation) s.pre = (const uint16_t*)pre->data, s.ldpre = stride_of(pre, M, N);
         if (b.dz) s.dz = (uint16_t*)dz;
-        if (dbias) s.sums = sums;
+        if (dbias) s.sums = b.sums ? sums : dbias;
         void* args[] = {&s};
         if (const int rc = launch(dtype ? (const void*)slope_kernel<BF16> : (const void*)slope_kernel<F16>, dim3(b.slope.blocks, b.slope.chunks), 256, args, stream))
             return rc;
-        if (dbias) {
+        if (b.sums) {
             const float* from = sums;
             int chunks = b.slope.chunks;
             void* list[] = {&from, &chunks, &N, &dbias};

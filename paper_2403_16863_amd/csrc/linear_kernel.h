@@ -140,6 +140,9 @@ struct Epilogue {
     const uint16_t* residual;  // or null
     uint16_t* pre;           // or null
     int ldr, ldp, bias_f32, act;
+    // Rows of pre begin on lines of 128 bytes: it is stored past the caches, for the backward pass reads it later (4096 x 16384 x 4096 437 -> 428 us; off the
+    // lines the parts of a line would go out by themselves, 7782 x 10248 x 648 236 us in place of 165).
+    int pre_lines;
 };
 
 struct Args {
@@ -190,8 +193,11 @@ __device__ __forceinline__ void finish(const Epilogue& e, uint16_t* out, int ldo
 #pragma unroll
         for (int i = 0; i < W; ++i) v[i] += bias[i];
     }
-    if (e.pre)  // (past the caches, for the backward pass: 4096 x 16384 x 4096 437 -> 428 us)
-        __builtin_nontemporal_store(pack<T, W>(v), (Packed<W>*)(e.pre + (size_t)m * e.ldp + n));
+    if (e.pre) {
+        Packed<W>* const to = (Packed<W>*)(e.pre + (size_t)m * e.ldp + n);
+        if (e.pre_lines) __builtin_nontemporal_store(pack<T, W>(v), to);
+        else *to = pack<T, W>(v);
+    }
     activate<W>(v, e.act);
     if (e.residual) {
         float r[W];
