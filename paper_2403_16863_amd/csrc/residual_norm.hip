@@ -17,6 +17,7 @@
 #include "../../include/residual_norm.h"
 #include "kv4_format.h"
 #include "memory_check.h"
+#include "turns.h"
 
 namespace stream_norm {
 
@@ -238,9 +239,8 @@ __global__ __launch_bounds__(Block<W>::threads) void backward_kernel(Args a) {
     const float mean = 1.f / (float)a.C;
     int at = 0;
     float* const sums = a.sums ? a.sums + (long long)blockIdx.x * 2 * a.C : nullptr;
-    const int units = a.runs * a.chunks;
-    for (int unit = blockIdx.x; unit < units; unit += gridDim.x) {
-        const int run = unit / a.chunks;
+    for (Turns turn = {blockIdx.x, gridDim.x, (unsigned)a.runs * (unsigned)a.chunks}; turn.left(); turn.next()) {
+        const int unit = (int)turn.at, run = unit / a.chunks;
         const long long base = (long long)run * a.length, first = (long long)(unit - run * a.chunks) * a.rows;
         const long long end = min((long long)a.length, first + a.rows);
         if (unit == (int)blockIdx.x || by_sequence) {
