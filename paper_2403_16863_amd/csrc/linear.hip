@@ -356,17 +356,23 @@ static int backward(const linear_rows* dy, const linear_rows* x, const linear_ro
     const Backward b = backward_of(M, N, K, w_rows_of_n, dw_rows_of_n, activation, want_x, want_w, dbias);
     if (b.dx.tile < 0 || b.dw.tile < 0 || (long long)b.slope.blocks * b.slope.chunks * 256 > (long long)UINT_MAX || b.slope.chunks > 65535)
         return LINEAR_EUNSUPPORTED;
-    void* const workspace = b.total() ? memory.take(b.total()) : nullptr;
-    if (b.total() && !workspace) return LINEAR_ENOMEM;
     const Rows2D in[] = {block(dy, M, N), activation ? block(pre, M, N) : Rows2D{}, want_w ? block(x, M, K) : Rows2D{},
                          want_x ? block(w, wr, wc) : Rows2D{}};
-    const Rows2D out[] = {want_x ? block(dx, M, K) : Rows2D{}, want_w ? block(dw, dwr, dwc) : Rows2D{}, vector_of(dbias, 4ll * N),
-                          b.total() ? vector_of(workspace, b.total()) : Rows2D{}};
-    for (int i = 0; i < 4; ++i) {
+    const Rows2D out[] = {want_x ? block(dx, M, K) : Rows2D{}, want_w ? block(dw, dwr, dwc) : Rows2D{}, vector_of(dbias, 4ll * N)};
+    for (int i = 0; i < 3; ++i) {
         for (const Rows2D& t : in)
             if (rows_meet(out[i], t)) return LINEAR_EINVAL;
         for (int j = 0; j < i; ++j)
             if (rows_meet(out[i], out[j])) return LINEAR_EINVAL;
+    }
+    void* const workspace = b.total() ? memory.take(b.total()) : nullptr;
+    if (b.total()) {
+        if (!workspace) return LINEAR_ENOMEM;
+        const Rows2D mine = vector_of(workspace, b.total());
+        for (const Rows2D& t : in)
+            if (rows_meet(mine, t)) return LINEAR_EINVAL;
+        for (const Rows2D& t : out)
+            if (rows_meet(mine, t)) return LINEAR_EINVAL;
     }
     char* const dz = (char*)workspace;
     float* const sums = (float*)(dz + b.dz);

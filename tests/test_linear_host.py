@@ -106,6 +106,23 @@ def test_memory_asked_for_by_the_call():
     assert L.gemm_linear_with(NONE, *args[1:]) == linear.LINEAR_EINVAL and L.gemm_linear_bwd_with(NONE, *back[1:]) == linear.LINEAR_EINVAL and not asked
 
 
+def test_no_memory_is_asked_for_by_calls_that_are_refused():
+    """Neither for bad arguments nor for outputs over other memory: the overlap is what the caller hears of, not the missing memory."""
+    asked = []
+    fn, L = linear.SCRATCH_FN(lambda owner, n: asked.append(n)), linear.lib()
+
+    def ask(dy=m(0x10000), x=m(0x20000), w=m(0x30000, 32), pre=m(0x40000), dx=m(0x50000), dw=m(0x60000, 32), dbias=0x70000, N=32, act=1):
+        return L.gemm_linear_bwd_with(dy, x, w, 0, pre, dx, dw, 0, p(dbias), act, 5, N, 64, 0, fn, None, None)
+    for bad in (dict(dx=m(0x10000)), dict(dx=m(0x20000)), dict(dx=m(0x60000)), dict(dw=m(0x20000, 32)), dict(dw=m(0x40000, 32)), dict(dbias=0x60000),
+                dict(dbias=0x10000), dict(dx=m(0x70000 - 16)), dict(N=12), dict(act=5), dict(pre=NONE), dict(dx=m(0x50008))):
+        assert ask(**bad) == linear.LINEAR_EINVAL and not asked, bad
+    assert ask() == linear.LINEAR_ENOMEM and len(asked) == 1
+    for bad in (dict(out=m(0x1000000, 64)), dict(out=m(0x2000000, 64)), dict(pre=m(0x3000000, 64)), dict(res=m(0x3000000 + 16, 64))):
+        t = {"out": m(0x3000000, 64), "pre": NONE, "res": NONE, **bad}
+        rc = L.gemm_linear_with(m(0x1000000, 16384), m(0x2000000, 64), 0, None, 0, t["res"], t["pre"], t["out"], 0, 4, 64, 16384, 0, fn, None, None)
+        assert rc == linear.LINEAR_EINVAL and len(asked) == 1, bad
+
+
 def test_products_refuse_bad_arguments():
     L = linear.lib()
 
