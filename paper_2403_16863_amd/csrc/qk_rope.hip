@@ -148,6 +148,11 @@ __global__ __launch_bounds__(256, 4) void rope_kernel(ARGS a) {
             const uint16_t* x = T.x + b * T.xs[0] + n * T.xs[1];
             const uint16_t* dy = T.dy + b * T.dys[0] + n * T.dys[1];
             uint16_t* y = T.y + b * T.ys[0] + n * T.ys[1];
+            // A pair without an axis stays as it is: turned by 1 and 0 an infinity would be NaN in its neighbour, and a zero could lose its sign.
+            auto turned = [&](int i) __attribute__((always_inline)) {
+                if constexpr (std::is_same_v<ARGS, AxesArgs>) return (a.axis[l] >> 4 * i & 15) != kNoAxis;
+                return true;
+            };
             for (int h = from + phase; h < to; h += PHASES) {
                 float v[16], g[16], r = 1;
                 if (!BACK || T.w) {
@@ -171,8 +176,8 @@ __global__ __launch_bounds__(256, 4) void rope_kernel(ARGS a) {
                     for (int i = 0; i < 8; ++i) {
                         const int p = PAIRS ? 2 * i : i, q = PAIRS ? 2 * i + 1 : i + 8;
                         const float m = v[p] * w[p], k = v[q] * w[q];
-                        v[p] = m * c[i] - k * s[i];
-                        v[q] = k * c[i] + m * s[i];
+                        v[p] = turned(i) ? m * c[i] - k * s[i] : m;
+                        v[q] = turned(i) ? k * c[i] + m * s[i] : k;
                     }
                     store8<BF>(y + h * T.ys[2] + lo, v);
                     store8<BF>(y + h * T.ys[2] + hi, v + 8);
@@ -181,8 +186,8 @@ __global__ __launch_bounds__(256, 4) void rope_kernel(ARGS a) {
                     for (int i = 0; i < 8; ++i) {
                         const int p = PAIRS ? 2 * i : i, q = PAIRS ? 2 * i + 1 : i + 8;
                         const float m = g[p] * c[i] + g[q] * s[i];
-                        g[q] = g[q] * c[i] - g[p] * s[i];
-                        g[p] = m;
+                        g[q] = turned(i) ? g[q] * c[i] - g[p] * s[i] : g[q];
+                        g[p] = turned(i) ? m : g[p];
                     }
                     if (T.w) {
                         float dot = 0;
