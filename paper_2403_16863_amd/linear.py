@@ -292,6 +292,8 @@ def linear_product(a, b, layout: int, c, tile: int, ranges: int = 1, workspace=N
     """c [M,N] <- the product of a and b as they lie in memory on tile `tile` with k in `ranges` parts, for tests and measurement: a [M,K], b
     [K,N] (ROWS); a [M,K], b [N,K] (ROWS_N); a [K,M], b [K,N] (TOKENS).  ranges > 1: workspace of ranges * M * N * 4 bytes."""
     import torch
+    if layout not in (ROWS, ROWS_N, TOKENS):
+        raise ValueError("layout must be ROWS, ROWS_N or TOKENS")
     for name, t in (("a", a), ("b", b), ("c", c)):
         if t.dim() != 2:
             raise ValueError(f"{name} must be a matrix")
@@ -301,6 +303,8 @@ def linear_product(a, b, layout: int, c, tile: int, ranges: int = 1, workspace=N
     _matrix("c", c, (M, N), a)
     _fit("linear_product", M, N, K)
     rows = [_rows(name, t) for name, t in (("a", a), ("b", b), ("c", c))]
+    if workspace is not None:
+        _check_workspace(workspace, 0, a)       # (how much the ranges need, the library knows)
     with torch.cuda.device(a.device):
         rc = lib().linear_product(rows[0], rows[1], int(layout), rows[2], M, N, K, _dtype(a), int(tile), int(ranges), _ptr(workspace),
                                   0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream, a.device))

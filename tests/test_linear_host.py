@@ -180,3 +180,19 @@ def test_python_names_what_it_refuses():
     for call, count in ((n.gemm_linear, 9), (n.gemm_linear_bwd, 10)):
         for args in ((), (t,) * count, (None,) * count, (1,) * count):
             assert call(*args) == n.NOT_PLAIN
+
+
+def test_products_in_python_refuse_memory_that_they_cannot_use():
+    """A workspace in host memory or with gaps, or a layout that is none, never reaches the library."""
+    from torch._subclasses.fake_tensor import FakeTensorMode
+    with FakeTensorMode():
+        def e(*shape, dtype=torch.float16, device="cuda"):
+            return torch.empty(*shape, dtype=dtype, device=device)
+        a, b, c = e(4, 512), e(512, 16), e(4, 16)
+        space = 2 * 4 * 16 * 4
+        for bad in (e(space, dtype=torch.uint8, device="cpu"), e(space, 2, dtype=torch.uint8)[:, 0]):
+            with pytest.raises(ValueError, match="workspace"):
+                linear.linear_product(a, b, linear.ROWS, c, 0, 2, bad, stream=0)
+        for layout in (-1, 3, 1.5):
+            with pytest.raises(ValueError, match="layout"):
+                linear.linear_product(a, b, layout, c, 0, stream=0)
