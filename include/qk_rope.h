@@ -51,7 +51,7 @@ int qk_norm_rope(const qk_heads* q, const qk_heads* k, const qk_heads* q_out, co
 
 /* dq, dk, dq_weight, dk_weight <- gradients, from dq_out, dk_out and the forward's q, k.  A tensor without a weight needs no q (k)
  * and has no weight gradient.
- *  dq_weight, dk_weight : device, fp32 [d], written (not added to); one for each weight.
+ *  dq_weight, dk_weight : device, fp32 [d], written (not added to); one for each weight, which overlap nothing.
  *  workspace : needed where there is a weight: device, 16-byte aligned, qk_norm_rope_bwd_workspace bytes, any contents, not used by
  *              anybody else until the call's kernels have run.
  * dq may be dq_out's own memory with the same strides.  The order of all sums is fixed by the sizes: results do not change from run to run. */

@@ -13,6 +13,7 @@
 
 #include "../../include/qk_rope.h"
 #include "kv4_format.h"
+#include "memory_check.h"
 
 namespace qk {
 
@@ -370,7 +371,15 @@ int backward(const qk_heads* dq_out, const qk_heads* dk_out, const qk_heads* q, 
     if (const int rc = check(B, N, H, Hkv, d)) return rc;
     const Grid g = grid_of((long long)B * N, H + Hkv, d, true);
     const bool sums = q_weight || k_weight;
-    if (sums && (!workspace || (uintptr_t)workspace % 16 || workspace_bytes < (long long)g.x * g.y * 2 * d * 4)) return QK_EINVAL;
+    const long long need = (long long)g.x * g.y * 2 * d * 4;
+    if (sums && (!workspace || (uintptr_t)workspace % 16 || workspace_bytes < need)) return QK_EINVAL;
+    // the weights' gradients lie apart, and the sums that they are added from apart from them and from the weights
+    const unsigned long long grad = 4ull * d, weight = (weight_f32 ? 4ull : 2ull) * d;
+    if (bytes_meet(dq_weight, grad, dk_weight, grad)) return QK_EINVAL;
+    for (const float* t : {dq_weight, dk_weight})
+        if (sums && bytes_meet(workspace, need, t, grad)) return QK_EINVAL;
+    for (const void* t : {q_weight, k_weight})
+        if (sums && bytes_meet(workspace, need, t, weight)) return QK_EINVAL;
     AxesArgs a = {};
     if (axes && !fill(&a, *axes, d)) return QK_EINVAL;
     const qk_heads* x[2] = {q, k};

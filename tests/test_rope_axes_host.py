@@ -42,6 +42,22 @@ def test_refusals():
                 assert call(**good) == rope.QK_ELAUNCH
 
 
+def test_gradients_of_weights_over_other_memory_are_refused():
+    """One tensor for both weights' gradients, or the sums' own memory, in both forms of the call."""
+    def call(by_axes, dqw=0x92000, dkw=0x93000, qw=0x90000, kw=0x91000, f32=0, ws=0xa0000):
+        L, more = rope.lib(), (3, GOOD) if by_axes else ()
+        return (L.qk_norm_rope_axes_bwd if by_axes else L.qk_norm_rope_bwd)(
+            h(0x10000), h(0x20000), h(0x30000), h(0x40000), h(0x50000), h(0x58000), p(qw), p(kw), f32, p(dqw), p(dkw), p(0x60000), p(0x70000), p(0x80000), 9, *more,
+            1e-6, 0, 2, 3, 4, 2, 64, 0, p(ws), 1 << 30, None)
+    for by_axes in (False, True):
+        for bad in (dict(dkw=0x92000), dict(dkw=0x92000 + 252), dict(dqw=0x93000 + 4), dict(ws=0x92000), dict(ws=0x93000 - 16), dict(ws=0x90000), dict(ws=0x91000 + 112),
+                    dict(ws=0x91000 + 240, f32=1)):
+            assert call(by_axes, **bad) == rope.QK_EINVAL, bad
+        if not torch.cuda.is_available():
+            for good in (dict(), dict(dkw=0x92000 + 256), dict(ws=0x91000 + 128), dict(ws=0x91000 + 256, f32=1)):
+                assert call(by_axes, **good) == rope.QK_ELAUNCH, good
+
+
 def test_axes_of_pairs():
     assert rope.axes_of_pairs((1, 2, 3), 16) == bytes([0, 1, 1, 2, 2, 2, 255, 255])
     assert rope.axes_of_pairs((1, 2, 3), 16, alternating=True) == bytes([0, 1, 2, 1, 2, 2, 255, 255])
