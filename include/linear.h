@@ -13,7 +13,7 @@
  * General rules (those of attn.h): device pointers are the caller's, nothing is allocated, cleared or waited for, calls are asynchronous
  * on `stream` and may be recorded into a graph; LINEAR_OK or a negative error comes back.  On LINEAR_EINVAL and LINEAR_EUNSUPPORTED nothing has
  * been enqueued.  After LINEAR_ELAUNCH earlier kernels of the call may have been: its memory is in use until the stream has run, and what
- * it writes is undefined.  No C++ exception crosses this boundary.  The order of all sums is fixed by the sizes, the weight's layout and whether there is a
+ * it writes is undefined.  No C++ exception crosses this boundary.  The order of all sums is fixed by the sizes, the layouts of w and dw and whether there is a
  * workspace: results do not change from run to run.
  */
 #ifndef PAPER_2403_16863_AMD_LINEAR_H

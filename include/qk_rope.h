@@ -64,7 +64,7 @@ int qk_norm_rope_bwd(const qk_heads* dq_out, const qk_heads* dk_out, const qk_he
  * token's position on the pair's own axis names.
  *  positions    : device, int32 [B, N, axes], axes 1 .. 4; one outside 0 .. rows-1 makes the outputs (backward: gradients) of that axis's pairs NaN (backward
  *                 with a weight: of all pairs of the token).
- *  axis_of_pair : HOST, d/2 values, read before the call returns: the axis of each pair, 0 .. axes-1, or QK_NO_AXIS for a pair that is not turned. */
+ *  axis_of_pair : HOST, d/2 values, read before the call returns: the axis of each pair, 0 .. axes-1, or QK_NO_AXIS for a pair that is not turned (y = n). */
 #define QK_NO_AXIS 255
 int qk_norm_rope_axes(const qk_heads* q, const qk_heads* k, const qk_heads* q_out, const qk_heads* k_out, const void* q_weight,
                       const void* k_weight, int weight_f32, const float* cos, const float* sin, const int* positions, int rows, int axes,

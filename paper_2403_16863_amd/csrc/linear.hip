@@ -32,6 +32,8 @@ __global__ __launch_bounds__(64) void join_kernel(const float* parts, Args p, in
 
 // dz = dy act'(pre), rounded, and the rows' sums for dbias, in one pass over dy and pre: memory binds.  A workgroup has 256 / lanes rows of `lanes` vectors of 8
 // columns (a power of two, 64 at most) and goes through a chunk of the rows; its sums meet in LDS in a fixed order.
+// dz is held in the matrices' 16 bits: products of 32 bits run at a fifteenth of the rate, and dz in two parts of 16 bits would be both products twice.
+// The gradients' error against 64 bits is 1.4 times that of the result's own rounding for it (2.3e-3 in bfloat16, 2.9e-4 in binary16).
 struct SlopeArgs {
     const uint16_t *dy, *pre;
     uint16_t* dz;

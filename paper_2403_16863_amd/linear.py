@@ -226,7 +226,8 @@ def gemm_linear_bwd_workspace(M: int, N: int, K: int, activation: str = "none", 
 def gemm_linear_bwd(dy, x, w, pre=None, dx=None, dw=None, dbias=None, activation: str = "none", workspace=None, stream=None) -> None:
     """dx, dw, dbias <- gradients of gemm_linear from out's gradient dy [M,N]: dz = dy act'(pre), dx [M,K] = dz @ w.T, dw [K,N] = x.T @ dz,
     dbias (float32 [N]) = dz's sum over the rows.  Those that are None are left out, and so may be w without dx and x without dw; pre, the forward's,
-    is needed with an activation.  dw may be the transposed view of [N,K], whichever w is.  The residual's gradient is dy itself.  All are written,
+    is needed with an activation.  dw may be the transposed view of [N,K], whichever w is.  With an activation dz is rounded to
+    the matrices' type ahead of both products, and not for dbias.  The residual's gradient is dy itself.  All are written,
     none added to, and overlap nothing.
     The call needs scratch memory in most cases: `workspace` (uint8, gemm_linear_bwd_workspace bytes), or, on torch's current stream, memory that it
     takes from torch's allocator itself (the graph's own pool while torch records one).  On another stream, and in a recording begun
